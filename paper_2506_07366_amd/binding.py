@@ -2,7 +2,7 @@
 
 Every function takes torch tensors that already live on the GPU, checks dtype /
 contiguity / device, passes raw device pointers and the current HIP stream to the
-C ABI declared in ``include/moegps.h`` and raises ``MoeGpsError`` on a non-zero
+C ABI declared in ``include/moegps.h`` and ``include/moegps_train.h`` and raises ``MoeGpsError`` on a non-zero
 return code.  There is no CPU fallback: if the shared library has not been built
 the first call raises.
 """
@@ -31,6 +31,8 @@ EXPORTS = [
     "moe_combine", "moe_comm_matrix", "moe_predictor_update", "moe_predictor_predict",
     "moe_packed_weights_relu_bytes", "moe_pack_weights_relu", "moe_grouped_ffn_relu", "moe_layer_step",
 ]
+# declared in include/moegps_train.h
+EXPORTS_TRAIN = ["moe_checkpoint_store", "moe_checkpoint_load", "moe_combine_backward"]
 
 
 class MoeGpsError(RuntimeError):
@@ -106,6 +108,12 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.moe_comm_matrix.argtypes = [c_int, c_int, c_int, c_int, c_int, vp, vp, vp, vp, vp, vp, vp]
     lib.moe_layer_step.restype = c_int
     lib.moe_layer_step.argtypes = [ctypes.c_char_p, vp]
+    lib.moe_combine_backward.restype = c_int
+    lib.moe_combine_backward.argtypes = [vp, c_int, c_int, c_int, c_int, c_int, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+    lib.moe_checkpoint_store.restype = c_int
+    lib.moe_checkpoint_store.argtypes = [vp, c_int, c_i64, c_int, vp, vp, vp]
+    lib.moe_checkpoint_load.restype = c_int
+    lib.moe_checkpoint_load.argtypes = [vp, vp, c_i64, c_int, vp, c_int, vp]
     if path is None:
         _lib = lib
     return lib
@@ -403,6 +411,94 @@ def moe_combine(y_perm: torch.Tensor, row_of_assign: torch.Tensor, topk_w: Optio
     _check(lib.moe_combine(_ptr(y_perm), dt, T, d, k, _ptr(row_of_assign), _ptr(topk_w), _ptr(out), _stream()),
            "moe_combine")
     return out
+
+
+CHECKPOINT_GROUP = 32  # values of a row that share a scale
+
+
+def _need_shape(t: torch.Tensor, shape, name: str) -> torch.Tensor:
+    if tuple(t.shape) != tuple(shape):
+        raise MoeGpsError(f"{name} must be {list(shape)}, got {list(t.shape)}")
+    return t
+
+
+def _need_checkpoint(kept, rows: int, d: int, name: str):
+    """(codes, scales) of a checkpoint of ``rows`` rows of ``d`` values."""
+    codes, scales = kept
+    if codes.dtype != torch.uint8:
+        _need(codes, torch.float8_e4m3fn, f"{name} codes")
+    _need(codes, codes.dtype, f"{name} codes")
+    _need(scales, torch.uint8, f"{name} scales")
+    _need_shape(codes, (rows, d), f"{name} codes")
+    _need_shape(scales, (rows, -(-d // CHECKPOINT_GROUP)), f"{name} scales")
+    return codes, scales
+
+
+def moe_checkpoint_store(x: torch.Tensor, out=None):
+    """Rows kept in 8 bits: (codes [rows, d] float8_e4m3fn, scales [rows, ceil(d / 32)] uint8, biased exponents).
+    ``out``: optional (codes, scales) to write into."""
+    lib = load_library()
+    dt = dtype_code(x)
+    _need(x, x.dtype, "x")
+    rows, d = x.shape
+    if out is None:
+        out = (torch.empty((rows, d), dtype=torch.float8_e4m3fn, device=x.device),
+               torch.empty((rows, -(-d // CHECKPOINT_GROUP)), dtype=torch.uint8, device=x.device))
+    codes, scales = _need_checkpoint(out, rows, d, "out")
+    _check(lib.moe_checkpoint_store(_ptr(x), dt, rows, d, _ptr(codes), _ptr(scales), _stream()), "moe_checkpoint_store")
+    return codes, scales
+
+
+def moe_checkpoint_load(codes: torch.Tensor, scales: torch.Tensor, dtype: torch.dtype,
+                        out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The rows that a checkpoint stands for."""
+    lib = load_library()
+    rows, d = codes.shape
+    _need_checkpoint((codes, scales), rows, d, "the")
+    if out is None:
+        out = torch.empty((rows, d), dtype=dtype, device=codes.device)
+    _need_shape(_need(out, dtype, "out"), (rows, d), "out")
+    _check(lib.moe_checkpoint_load(_ptr(codes), _ptr(scales), rows, d, _ptr(out), dtype_code(out), _stream()),
+           "moe_checkpoint_load")
+    return out
+
+
+def moe_combine_backward(dout: torch.Tensor, y_perm, row_of_assign: torch.Tensor, topk_w: torch.Tensor,
+                         topk_idx: Optional[torch.Tensor] = None, E: int = 0, out=None):
+    """(dy_perm, dtopk_w, dlogits): gradients of the rows of y_perm, of the gate weights and, given ``topk_idx`` and
+    ``E``, of the router logits (else None).  ``y_perm``: the rows, their checkpoint (codes, scales), or None (only
+    dy_perm is wanted).  ``out``: optional (dy_perm, dtopk_w, dlogits) to write into; dy_perm may be y_perm."""
+    lib = load_library()
+    dt = dtype_code(dout)
+    _need(dout, dout.dtype, "dout")
+    T, d = dout.shape
+    k = _need(topk_w, torch.float32, "topk_w").shape[1]
+    _need_shape(topk_w, (T, k), "topk_w")
+    A = T * k
+    if _need(row_of_assign, torch.int32, "row_of_assign").numel() != A:
+        raise MoeGpsError("row_of_assign must have one entry per assignment")
+    scales = None
+    if isinstance(y_perm, (tuple, list)):
+        y_perm, scales = _need_checkpoint(y_perm, A, d, "y_perm")
+    elif y_perm is not None:
+        _need_shape(_need(y_perm, dout.dtype, "y_perm"), (A, d), "y_perm")
+    if topk_idx is not None:
+        _need_shape(_need(topk_idx, torch.int32, "topk_idx"), (T, k), "topk_idx")
+    if out is None:
+        dy = torch.empty((A, d), dtype=dout.dtype, device=dout.device)
+        dw = None if y_perm is None else torch.empty((T, k), dtype=torch.float32, device=dout.device)
+        dl = None if topk_idx is None else torch.empty((T, E), dtype=torch.float32, device=dout.device)
+    else:
+        dy, dw, dl = out
+    _need_shape(_need(dy, dout.dtype, "dy_perm"), (A, d), "dy_perm")
+    if dw is not None:
+        _need_shape(_need(dw, torch.float32, "dtopk_w"), (T, k), "dtopk_w")
+    if dl is not None:
+        _need_shape(_need(dl, torch.float32, "dlogits"), (T, E), "dlogits")
+    _check(lib.moe_combine_backward(_ptr(dout), dt, T, d, k, E, _ptr(row_of_assign), _ptr(topk_w), _ptr(topk_idx),
+                                    _ptr(y_perm), _ptr(scales), _ptr(dy), _ptr(dw), _ptr(dl), _stream()),
+           "moe_combine_backward")
+    return dy, dw, dl
 
 
 def moe_comm_matrix(mode: int, topk_idx: torch.Tensor, pred_idx: Optional[torch.Tensor],
