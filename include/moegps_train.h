@@ -60,6 +60,48 @@ int moe_combine_backward(const void* dout, int dtype, int T, int d, int k, int E
                          const float* topk_w, const int32_t* topk_idx, const void* y_perm, const uint8_t* y_scales,
                          void* dy_perm, float* dtopk_w, float* dlogits, void* stream);
 
+/*
+ * Gradient of the grouped expert FFN (moe_grouped_ffn and its forms; relu: moe_grouped_ffn_relu).  For every row r of a
+ * segment, with e = slot_expert of it, x_r = x[assign_of_row[r] / k] and dy_r = dy_perm[r]:
+ *     a = x_r W1_e, b = x_r W3_e, s = 1 / (1 + exp(-a)), h = a s b       relu: h = max(a, 0)
+ *     dh = dy_r W2_e^T,  da = dh b s (1 + a (1 - s)),  db = dh a s       relu: da = dh where a > 0, else 0
+ *     dx_perm[r] = da W1_e^T + db W3_e^T                                 relu: da W1_e^T
+ *     dW1_e = sum_r x_r^T da,  dW3_e = sum_r x_r^T db,  dW2_e = sum_r h^T dy_r
+ * over all rows of the expert, its replicas' among them.  The hidden activations are worked out again from x, so the forward
+ * pass keeps nothing but x.
+ *   x          [T, d] dtype in, or with x_scales the codes of a checkpoint of it (moe_checkpoint_store)
+ *   assign_of_row [T*k], seg_offsets [nseg + 1], slot_expert [nseg] int32 in, as in the forward pass
+ *   packed     in, from moe_pack_weights (relu: moe_pack_weights_relu)
+ *   packed_backward  in, from moe_pack_weights_backward; not read with MOE_DTYPE_F32
+ *   dy_perm    [T*k, d] dtype in
+ *   dx_perm    [T*k, d] dtype out, rows of segments whose slot holds no expert are not written; NULL: not wanted
+ *   dW1, dW3 [E, d, ffn], dW2 [E, ffn, d] dtype out, written whole (zeros for experts without rows); NULL, all of them: not
+ *              wanted.  dW3 is NULL with relu
+ * bf16: sums in fp32; dh, h, da and db are rounded to bf16 as operands of the next products, results once.  The result does
+ * not depend on the order in which parts of the launch run.  Outputs and workspace overlap nothing.
+ * bf16 needs d % 64 == 0 and T*k*d < 2^31, f32 d % 4 == 0 and ffn % 4 == 0; limits otherwise as in the forward pass.
+ * T = 0 writes zeros to the weight gradients.  Arguments are checked before the first launch.
+ *
+ * moe_pack_weights_backward lays the weights out for the products with transposed weights, like moe_pack_weights whenever they have
+ * changed (W3 NULL: the ReLU form).  Nothing to do for MOE_DTYPE_F32, whose size is 0.
+ */
+typedef struct moe_ffn_backward_args {
+    int32_t dtype, T, k, d, ffn, E, nseg, relu;
+    const void* x;
+    const uint8_t* x_scales;
+    const int32_t *assign_of_row, *seg_offsets, *slot_expert;
+    const void *packed, *packed_backward;
+    const void* dy_perm;
+    void *dx_perm, *dW1, *dW3, *dW2;
+    void* workspace;
+    size_t workspace_bytes;
+} moe_ffn_backward_args;
+size_t moe_packed_weights_backward_bytes(int E, int d, int ffn, int dtype, int relu);
+int moe_pack_weights_backward(const void* W1, const void* W3, const void* W2, int dtype, int E, int d, int ffn,
+                              void* packed, void* stream);
+size_t moe_grouped_ffn_backward_workspace_bytes(int T, int k, int d, int ffn, int E, int nseg, int dtype, int relu);
+int moe_grouped_ffn_backward(const moe_ffn_backward_args* args, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -32,7 +32,10 @@ EXPORTS = [
     "moe_packed_weights_relu_bytes", "moe_pack_weights_relu", "moe_grouped_ffn_relu", "moe_layer_step",
 ]
 # declared in include/moegps_train.h
-EXPORTS_TRAIN = ["moe_checkpoint_store", "moe_checkpoint_load", "moe_combine_backward"]
+EXPORTS_TRAIN = [
+    "moe_checkpoint_store", "moe_checkpoint_load", "moe_combine_backward", "moe_packed_weights_backward_bytes",
+    "moe_pack_weights_backward", "moe_grouped_ffn_backward_workspace_bytes", "moe_grouped_ffn_backward",
+]
 
 
 class MoeGpsError(RuntimeError):
@@ -114,6 +117,14 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.moe_checkpoint_store.argtypes = [vp, c_int, c_i64, c_int, vp, vp, vp]
     lib.moe_checkpoint_load.restype = c_int
     lib.moe_checkpoint_load.argtypes = [vp, vp, c_i64, c_int, vp, c_int, vp]
+    lib.moe_packed_weights_backward_bytes.restype = c_sz
+    lib.moe_packed_weights_backward_bytes.argtypes = [c_int] * 5
+    lib.moe_pack_weights_backward.restype = c_int
+    lib.moe_pack_weights_backward.argtypes = [vp, vp, vp, c_int, c_int, c_int, c_int, vp, vp]
+    lib.moe_grouped_ffn_backward_workspace_bytes.restype = c_sz
+    lib.moe_grouped_ffn_backward_workspace_bytes.argtypes = [c_int] * 8
+    lib.moe_grouped_ffn_backward.restype = c_int
+    lib.moe_grouped_ffn_backward.argtypes = [ctypes.c_char_p, vp]
     if path is None:
         _lib = lib
     return lib
@@ -499,6 +510,77 @@ def moe_combine_backward(dout: torch.Tensor, y_perm, row_of_assign: torch.Tensor
                                     _ptr(y_perm), _ptr(scales), _ptr(dy), _ptr(dw), _ptr(dl), _stream()),
            "moe_combine_backward")
     return dy, dw, dl
+
+
+def moe_packed_weights_backward_bytes(E: int, d: int, ffn: int, dtype: int, relu: bool = False) -> int:
+    return int(load_library().moe_packed_weights_backward_bytes(E, d, ffn, dtype, relu))
+
+
+def moe_pack_weights_backward(W1: torch.Tensor, W3: Optional[torch.Tensor], W2: torch.Tensor) -> torch.Tensor:
+    """Weights laid out for the backward pass (W3 None: the ReLU form); empty for fp32, which needs none."""
+    lib = load_library()
+    dt = dtype_code(W1)
+    for name, t in (("W1", W1), ("W3", W3), ("W2", W2)):
+        if t is not None:
+            _need(t, W1.dtype, name)
+    E, d, ffn = W1.shape
+    if (W3 is not None and tuple(W3.shape) != (E, d, ffn)) or tuple(W2.shape) != (E, ffn, d):
+        raise MoeGpsError("weight shapes must be W1,W3 [E,d,ffn] and W2 [E,ffn,d]")
+    packed = torch.empty(moe_packed_weights_backward_bytes(E, d, ffn, dt, W3 is None), dtype=torch.uint8,
+                         device=W1.device)
+    _check(lib.moe_pack_weights_backward(_ptr(W1), _ptr(W3), _ptr(W2), dt, E, d, ffn, _ptr(packed), _stream()),
+           "moe_pack_weights_backward")
+    return packed
+
+
+def moe_grouped_ffn_backward_workspace_bytes(T: int, k: int, d: int, ffn: int, E: int, nseg: int, dtype: int,
+                                             relu: bool = False) -> int:
+    return int(load_library().moe_grouped_ffn_backward_workspace_bytes(T, k, d, ffn, E, nseg, dtype, relu))
+
+
+# moe_ffn_backward_args: eight int32, then pointers and a size of eight bytes
+_FFN_BACKWARD_ARGS = struct.Struct("@8i14Q")
+
+
+def moe_grouped_ffn_backward(x, assign_of_row: torch.Tensor, k: int, dy_perm: torch.Tensor, seg_offsets: torch.Tensor,
+                             slot_expert: torch.Tensor, packed: torch.Tensor, packed_backward: torch.Tensor, E: int,
+                             ffn: int, relu: bool = False, workspace: Optional[torch.Tensor] = None, out=None):
+    """(dx_perm, dW1, dW3, dW2): gradients of the FFN's input rows and of the expert weights (dW3 None with ``relu``).
+    ``x``: [T, d], or its checkpoint (codes, scales).  ``out``: optional (dx_perm, dW1, dW3, dW2) to write into;
+    dx_perm None, or all of the weight gradients None: not wanted."""
+    lib = load_library()
+    dt = dtype_code(dy_perm)
+    _need(dy_perm, dy_perm.dtype, "dy_perm")
+    A, d = dy_perm.shape
+    if k < 1 or A % k != 0:
+        raise MoeGpsError("dy_perm must have k rows per token")
+    T = A // k
+    scales = None
+    if isinstance(x, (tuple, list)):
+        x, scales = _need_checkpoint(x, T, d, "x")
+    else:
+        _need_shape(_need(x, dy_perm.dtype, "x"), (T, d), "x")
+    if _need(assign_of_row, torch.int32, "assign_of_row").numel() != A:
+        raise MoeGpsError("assign_of_row must have one entry per row")
+    nseg = _need(slot_expert, torch.int32, "slot_expert").numel()
+    if _need(seg_offsets, torch.int32, "seg_offsets").numel() != nseg + 1:
+        raise MoeGpsError("seg_offsets must have one entry more than slot_expert")
+    shapes = (("dx_perm", (A, d)), ("dW1", (E, d, ffn)), ("dW3", (E, d, ffn)), ("dW2", (E, ffn, d)))
+    if out is None:
+        out = tuple(None if relu and name == "dW3" else torch.empty(shape, dtype=dy_perm.dtype, device=dy_perm.device)
+                    for name, shape in shapes)
+    for t, (name, shape) in zip(out, shapes):
+        if t is not None:
+            _need_shape(_need(t, dy_perm.dtype, name), shape, name)
+    if workspace is None:
+        workspace = torch.empty(moe_grouped_ffn_backward_workspace_bytes(T, k, d, ffn, E, nseg, dt, relu),
+                                dtype=torch.uint8, device=dy_perm.device)
+    p = _ptr
+    args = _FFN_BACKWARD_ARGS.pack(
+        dt, T, k, d, ffn, E, nseg, relu, p(x), p(scales) or 0, p(assign_of_row), p(seg_offsets), p(slot_expert), p(packed),
+        p(packed_backward), p(dy_perm), *(p(t) or 0 for t in out), p(workspace), workspace.numel())
+    _check(lib.moe_grouped_ffn_backward(args, _stream()), "moe_grouped_ffn_backward")
+    return tuple(out)
 
 
 def moe_comm_matrix(mode: int, topk_idx: torch.Tensor, pred_idx: Optional[torch.Tensor],

@@ -2,6 +2,7 @@
 // waits and register-to-register helpers, where the rows of a product live, the pieces of the row copy.
 #pragma once
 #include "ffn_tables.h"
+#include <atomic>
 #include <type_traits>
 #include <utility>
 
@@ -106,8 +107,12 @@ __device__ __forceinline__ float silu_f(float g) { return g * __builtin_amdgcn_r
 
 // EPI selects what happens to the accumulators before they are stored: kEpiNone (plain
 // product, optionally scaled per row), kEpiSwiglu (silu(gate) * up on interleaved column
-// pairs, half as many output columns), kEpiRelu (max(., 0)).
-constexpr int kEpiNone = 0, kEpiSwiglu = 1, kEpiRelu = 2;
+// pairs, half as many output columns), kEpiRelu (max(., 0)); in the backward pass (ffn_backward.hip)
+// kEpiSwigluGrad and kEpiReluGrad (the hidden activation and the gradients of what it is made of, from the
+// gradient of the hidden activation).
+constexpr int kEpiNone = 0, kEpiSwiglu = 1, kEpiRelu = 2, kEpiSwigluGrad = 3, kEpiReluGrad = 4;
+// the first products of the forward pass take a share of the row copy along
+constexpr bool epi_copies(int epi) { return epi == kEpiSwiglu || epi == kEpiRelu; }
 
 // Where the rows of a product live.  List position p of an M-tile is
 //   operand row  a_rows ? a_rows[p] : p, and then, with a_rows2, a_rows2[that] / a_div
@@ -175,5 +180,41 @@ __device__ __forceinline__ void store_pieces(const RowCopy& c, int first, int n,
         if (++q == per_row) q = 0;
     }
 }
+
+// ---------------------------------------------------------------------------
+// host side: what the forward and the backward pass share
+// ---------------------------------------------------------------------------
+// The bf16 kernels work on a hidden width padded to a multiple of 64: the packed weights
+// carry zero columns (W1, W3) and zero rows (W2) for the padding, so the padded hidden
+// activations are exact zeros and add nothing to the second product.
+// Widths above this are refused: it keeps every size computed on the host inside 64 bits and
+// every tile offset computed on the device inside 32.
+constexpr int kMaxWidth = 1 << 22;
+inline bool ffn_shape_in_range(int64_t A, int d, int ffn, int nseg, int dtype) {
+    return (dtype == MOE_DTYPE_F32 || dtype == MOE_DTYPE_BF16) && A >= 0 && A < (1ll << 31) && d >= 1 &&
+           d <= kMaxWidth && ffn >= 1 && ffn <= kMaxWidth && nseg >= 1 && nseg <= MOE_MAX_SEGMENTS;
+}
+
+inline int padded_ffn(int ffn, int dtype) {
+    return dtype == MOE_DTYPE_BF16 ? (int)align_up((size_t)ffn, 64) : ffn;
+}
+// rows of a packed bf16 weight matrix: whole tiles
+inline size_t packed_rows(size_t n) { return align_up(n, (size_t)kPackN); }
+// elements of one expert's packed matrices: the first product's n1 matrices, the second product's
+inline size_t packed_elems1(int n1, int d, int fp) { return packed_rows((size_t)n1 * fp) * d; }
+inline size_t packed_elems2(int d, int fp) { return packed_rows((size_t)d) * fp; }
+
+constexpr int kMinBM = 32;  // the lowest tile shape
+
+// A kernel that uses more LDS than the default limit: raised once per kernel (`raised`: bit per device).
+int raise_lds(const void* kern, size_t bytes, std::atomic<unsigned long long>& raised);
+// Weights of a product that tiles read past the caches where they share them with no other tile.
+bool past_caches(int E, size_t b_stride);
+// The table builder as a launch of its own, for A rows.
+int launch_tables(int64_t A, const int32_t* seg_offsets, const int32_t* slot_expert, const TableJob& job, hipStream_t st);
+// A plain product by tiles: C[c_rows[p], 0 .. N) = A[a_rows[p], 0 .. K) x packed weights, for the rows of a table.
+int launch_product(const bf16_t* A, int lda, const bf16_t* Bp, size_t b_stride, int E, bf16_t* C, int ldc,
+                   const MTile* tiles, const int32_t* counts, int32_t* queues, int N, int K, const RowMap& rm,
+                   hipStream_t st);
 
 }  // namespace moegps

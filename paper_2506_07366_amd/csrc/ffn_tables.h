@@ -160,6 +160,7 @@ struct TableJob {
     int32_t* queues;     // claim counters to set
     int n_queues;
     int32_t* left;       // both products in one launch: what the second waits for (ffn_tiles.h); null: a launch each
+    int32_t* bases;      // [E + 1] first list position of every expert, then the number of rows; null: not wanted
 };
 
 // LDS of a builder for up to MAXSEG segments and MAXE experts that makes NT tables.
@@ -253,6 +254,8 @@ __device__ __forceinline__ void build_tables(TableScratch<MAXSEG, MAXE, NT>& sh,
     auto list_base = [&](int e) { return srt_base[e_segs[e]]; };  // first list position of expert e
     if (block == 0 && job.left)
         for (int e = tid; e < E; e += blockDim.x) job.left[e] = -((list_base(e + 1) - list_base(e)) * job.t1.n_ntiles);
+    if (block == 0 && job.bases)
+        for (int e = tid; e <= E; e += blockDim.x) job.bases[e] = list_base(e);
     // wavefront j < NT prepares table first_table + j while the others fill in the row list
     auto spec_of = [&](int j) -> const TableSpec& { return first_table + j == 0 ? job.t1 : job.t2; };
     auto wanted = [&](int j) { return first_table + j < 2 && spec_of(j).tiles != nullptr; };

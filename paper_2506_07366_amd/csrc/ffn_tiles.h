@@ -29,7 +29,7 @@ constexpr int kCopyPieces = 6;     // pieces of the row copy that a wavefront ta
 constexpr size_t kStageLds = (size_t)3 * kTileMaxRows * kPackK * 2;
 // dynamic LDS of a workgroup: the stages, in the first product the copy's pieces, the number of the next tile
 template <int EPI>
-constexpr size_t kNextTileAt = kStageLds + (EPI != kEpiNone ? 8 * kCopyPieces * kCopyPieceLds : 0);
+constexpr size_t kNextTileAt = kStageLds + (epi_copies(EPI) ? 8 * kCopyPieces * kCopyPieceLds : 0);
 template <int EPI>
 constexpr size_t kTileLds = kNextTileAt<EPI> + 16;
 
@@ -79,8 +79,10 @@ __device__ __forceinline__ void tile_product(
     int N, int K, int group_n, bool past_caches, RowMap rm,
     float* __restrict__ partials,  // [slab][kPartRows][N] fp32 sums of entries that cover part of K (plain product, a launch of its own)
     RowCopy copy,                  // first product: rows to be copied besides, a share of them with every tile
-    int32_t* left) {               // [E] what the second product waits for, see above (LINK)
-    constexpr bool SWIGLU = EPI == kEpiSwiglu;
+    int32_t* left,                 // [E] what the second product waits for, see above (LINK)
+    bf16_t* hidden = nullptr) {    // backward pass: [rows, SWIGLU ? N/2 : N] gradient of the hidden activation in, the
+                                   //   hidden activation out
+    constexpr bool SWIGLU = EPI == kEpiSwiglu || EPI == kEpiSwigluGrad;
     constexpr int BN = kPackN, BK = kPackK, NW = 8;
     constexpr int ROW_BYTES = BK * 2;      // of an activation row in a stage
     constexpr int B_BYTES = BN * BK * 2;   // of a weight tile
@@ -116,7 +118,7 @@ __device__ __forceinline__ void tile_product(
     const int total = n_entries * n_ntiles;
     const int total_whole = n_whole * n_ntiles;
     int copy_share = 0;  // pieces of the row copy that go with a tile
-    if constexpr (EPI != kEpiNone)
+    if constexpr (epi_copies(EPI))
         if (copy.x_perm) copy_share = ceil_div(copy.T * ceil_div(copy.chunks, kWave), total > 0 ? total : 1);
     volatile __attribute__((address_space(3))) int& next_tile =
         *(volatile __attribute__((address_space(3))) int*)(__attribute__((address_space(3))) unsigned char*)(smem + kNextTileAt<EPI>);
@@ -190,7 +192,7 @@ __device__ __forceinline__ void tile_product(
         // and stored at the tile's start instead (one memory round trip more per tile) 1679, 8956,
         // 279; copied by workgroups behind those of the product, as these run out of tiles, 1665, 8707, 294.
         int copy_first = 0, copy_n = 0;  // this wavefront's pieces
-        if constexpr (EPI != kEpiNone) {
+        if constexpr (epi_copies(EPI)) {
             if (copy.x_perm) {
                 const int all = copy.T * ceil_div(copy.chunks, kWave), first = t_all * copy_share;
                 const int end = first + copy_share < all ? first + copy_share : all;
@@ -287,7 +289,7 @@ __device__ __forceinline__ void tile_product(
                 offA[i] = ((unsigned)r * (unsigned)lda + (unsigned)((slot ^ swz(row)) * 8)) * 2u;
             }
             if constexpr (LINK == kMakesRows) rows_stored();  // the previous tile's results have reached memory
-            if constexpr (EPI != kEpiNone)  // (behind the row list, whose wait would be for the pieces too)
+            if constexpr (epi_copies(EPI))  // (behind the row list, whose wait would be for the pieces too)
                 if (copy_n > 0)
                     request_pieces(copy, copy_first, copy_n, smem + kStageLds + wave * (kCopyPieces * kCopyPieceLds));
             bf16x8 w[D][2][2], af[R];
@@ -430,7 +432,81 @@ __device__ __forceinline__ void tile_product(
                 *(uint4*)at = make_uint4(px, py, qx, qy);
             }
         };
-        if constexpr (SWIGLU) {
+        if constexpr (EPI == kEpiSwigluGrad) {
+            // With a = x W1, b = x W3, s = 1 / (1 + exp(-a)) and the gradient dh of h = a s b:
+            //     db = dh a s,   da = dh b s (1 + a (1 - s)),
+            // stored side by side in the packed columns of a and b.  h goes where dh was: a wavefront has read all it needs of
+            // its columns before it writes to them (and all at once: one memory round trip).
+            const int f0 = n0 / 2 + (wave >> 1) * 32 + (wave & 1) * 16, c0 = n0 + (wave >> 1) * 64 + (wave & 1) * 16;
+            const int ldh = N / 2;
+            uint2 raw[TM_MAX];
+#pragma unroll
+            for (int i = 0; i < TM_MAX; ++i) {
+                const int row = i * 16 + l16e;
+                raw[i] = uint2{0u, 0u};
+                if ((i & ~1) * 16 < mt.rows && f0 < ldh)
+                    raw[i] = *(const uint2*)(hidden + (size_t)(mt.list0 + (row < mt.rows ? row : mt.rows - 1)) * ldh + f0 +
+                                             g16e * 4);
+            }
+#pragma unroll
+            for (int i = 0; i < TM_MAX; i += 2) {
+                if (i * 16 < mt.rows) {
+                    float h[2][4], da[2][4], db[2][4];
+#pragma unroll
+                    for (int q = 0; q < 2; ++q)
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            const unsigned word = c < 2 ? raw[i + q].x : raw[i + q].y;
+                            const float dh = __builtin_bit_cast(float, c & 1 ? word & 0xffff0000u : word << 16);
+                            const float a = acc[i + q][0][c], b = acc[i + q][1][c];
+                            const float s = __builtin_amdgcn_rcpf(1.0f + __expf(-a));
+                            const float as = a * s;
+                            h[q][c] = as * b;
+                            db[q][c] = dh * as;
+                            da[q][c] = dh * b * fmaf(as, 1.0f - s, s);
+                        }
+                    const int row = (i + (g16e >> 1)) * 16 + l16e;
+                    const bool on = row < mt.rows && f0 < ldh;
+                    const size_t at = (size_t)(mt.list0 + row);
+                    store_pair(h[0], h[1], hidden + at * ldh + f0 + (g16e & 1) * 8, on);
+                    store_pair(da[0], da[1], C + at * ldc + c0 + (g16e & 1) * 8, on);
+                    store_pair(db[0], db[1], C + at * ldc + c0 + 32 + (g16e & 1) * 8, on);
+                }
+            }
+        } else if constexpr (EPI == kEpiReluGrad) {
+            // a = x W1, h = max(a, 0), da = dh where a > 0 and 0 elsewhere (also at 0); h goes where dh was, as above.
+            const int col0 = n0 + wave * 32;
+            uint2 raw[TM_MAX][2];
+#pragma unroll
+            for (int i = 0; i < TM_MAX; ++i)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const int row = i * 16 + l16e;
+                    raw[i][j] = uint2{0u, 0u};
+                    if (i * 16 < mt.rows && col0 < N)
+                        raw[i][j] = *(const uint2*)(hidden + (size_t)(mt.list0 + (row < mt.rows ? row : mt.rows - 1)) * N +
+                                                    col0 + j * 16 + g16e * 4);
+                }
+#pragma unroll
+            for (int i = 0; i < TM_MAX; ++i) {
+                if (i * 16 < mt.rows) {
+                    float h[2][4], da[2][4];
+#pragma unroll
+                    for (int j = 0; j < 2; ++j)
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            const unsigned word = c < 2 ? raw[i][j].x : raw[i][j].y;
+                            const float a = acc[i][j][c];
+                            h[j][c] = fmaxf(a, 0.f);
+                            da[j][c] = a > 0.f ? __builtin_bit_cast(float, c & 1 ? word & 0xffff0000u : word << 16) : 0.f;
+                        }
+                    const bool on = i * 16 + l16e < mt.rows && col0 < N;
+                    const size_t at = (size_t)(mt.list0 + i * 16 + l16e);
+                    store_pair(h[0], h[1], hidden + at * N + col0 + g16e * 8, on);
+                    store_pair(da[0], da[1], C + at * ldc + col0 + g16e * 8, on);
+                }
+            }
+        } else if constexpr (SWIGLU) {
             const int col = n0 / 2 + (wave >> 1) * 32 + (wave & 1) * 16 + (g16e & 1) * 8;
 #pragma unroll
             for (int i = 0; i < TM_MAX; i += 2) {
@@ -504,7 +580,7 @@ __device__ __forceinline__ void tile_product(
                 }
             }
         }
-        if constexpr (EPI != kEpiNone)
+        if constexpr (epi_copies(EPI))
             if (copy_n > 0) store_pieces(copy, copy_first, copy_n, (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)smem + kStageLds + wave * (kCopyPieces * kCopyPieceLds));
         if constexpr (LINK == kMakesRows) {
             told_expert = mt.expert;

@@ -30,7 +30,6 @@
 //
 // fp32 path (small reference-precision configs): the fp32 matrix instruction, operands from memory.
 #include "ffn_device.h"
-#include <atomic>
 
 namespace moegps {
 
@@ -276,34 +275,12 @@ struct FfnWs {
     int split_all;      // every tile is split (tests)
 };
 
-constexpr int kMinBM = 32;  // the lowest tile shape
-
 // Process-wide overrides of the automatic choices (moe_grouped_ffn_set_option); -1 / 0 = automatic.
 static std::atomic<int> g_opt_tile1{-1}, g_opt_tile2{-1}, g_opt_split{-1}, g_opt_group_n{0}, g_opt_stream{-1};
 
 FfnOptions ffn_options() {
     return {g_opt_tile1.load(), g_opt_tile2.load(), g_opt_split.load(), g_opt_group_n.load(), g_opt_stream.load()};
 }
-
-// The bf16 kernels work on a hidden width padded to a multiple of 64: the packed weights
-// carry zero columns (W1, W3) and zero rows (W2) for the padding, so the padded hidden
-// activations are exact zeros and add nothing to the second product.
-// Widths above this are refused: it keeps every size computed on the host inside 64 bits and
-// every tile offset computed on the device inside 32.
-constexpr int kMaxWidth = 1 << 22;
-static inline bool ffn_shape_in_range(int64_t A, int d, int ffn, int nseg, int dtype) {
-    return (dtype == MOE_DTYPE_F32 || dtype == MOE_DTYPE_BF16) && A >= 0 && A < (1ll << 31) && d >= 1 &&
-           d <= kMaxWidth && ffn >= 1 && ffn <= kMaxWidth && nseg >= 1 && nseg <= MOE_MAX_SEGMENTS;
-}
-
-static inline int padded_ffn(int ffn, int dtype) {
-    return dtype == MOE_DTYPE_BF16 ? (int)align_up((size_t)ffn, 64) : ffn;
-}
-// rows of a packed bf16 weight matrix: whole tiles
-static inline size_t packed_rows(size_t n) { return align_up(n, (size_t)kPackN); }
-// elements of one expert's packed matrices: the first product's n1 matrices, the second product's
-static inline size_t packed_elems1(int n1, int d, int fp) { return packed_rows((size_t)n1 * fp) * d; }
-static inline size_t packed_elems2(int d, int fp) { return packed_rows((size_t)d) * fp; }
 
 // Whether (and how) the closing tiles of the second product are computed as parts of K.  It
 // pays when the product has only a few rounds of tiles per workgroup, so that the uneven end
@@ -410,10 +387,9 @@ static int copy_blocks(RowCopy& copy, int threads) {
     return (int)ceil_div64((int64_t)copy.T * copy.slices, (int64_t)copy.per_wave * (threads / kWave));
 }
 
-static bool past_caches(int E, size_t b_stride) { return (size_t)E * b_stride * sizeof(bf16_t) > kCachedWeights; }
+bool past_caches(int E, size_t b_stride) { return (size_t)E * b_stride * sizeof(bf16_t) > kCachedWeights; }
 
-// A kernel that uses more LDS than the default limit: raised once per kernel (`raised`: bit per device).
-static int raise_lds(const void* kern, size_t bytes, std::atomic<unsigned long long>& raised) {
+int raise_lds(const void* kern, size_t bytes, std::atomic<unsigned long long>& raised) {
     int dev = 0;
     (void)hipGetDevice(&dev);
     const unsigned long long bit = 1ull << (dev & 63);
@@ -439,6 +415,20 @@ static int launch_tiles(const bf16_t* A, int lda, const bf16_t* Bp, size_t b_str
     // 32 workgroups for each of the 8 XCDs; they claim tiles from `queues` (cleared by the table builder)
     hipLaunchKernelGGL(kern, dim3(kGemmGrid), dim3(512), kTileLds<EPI>, st, A, lda, Bp, b_stride, C, ldc, tiles, counts, queues, N, K,
                        group_n, past_caches(E, b_stride), rm, partials, copy);
+    return check_launch();
+}
+
+int launch_product(const bf16_t* A, int lda, const bf16_t* Bp, size_t b_stride, int E, bf16_t* C, int ldc,
+                   const MTile* tiles, const int32_t* counts, int32_t* queues, int N, int K, const RowMap& rm,
+                   hipStream_t st) {
+    return launch_tiles<kEpiNone>(A, lda, Bp, b_stride, E, C, ldc, tiles, counts, queues, N, K, kTileGroup, rm, nullptr,
+                                  RowCopy{}, st);
+}
+
+int launch_tables(int64_t A, const int32_t* seg_offsets, const int32_t* slot_expert, const TableJob& job, hipStream_t st) {
+    // one position of the row list per thread up to 256 workgroups
+    const int grid = (int)(A <= 1024 ? 2 : (A > 255 * 1024 ? 256 : ceil_div64(A, 1024) + 1));
+    hipLaunchKernelGGL(build_tables_kernel, dim3(grid), dim3(1024), 0, st, seg_offsets, slot_expert, job);
     return check_launch();
 }
 
@@ -687,8 +677,6 @@ int grouped_ffn_call(int relu, const void* x_in, int64_t rows_in, const int32_t*
     hipStream_t st = (hipStream_t)stream;
     const size_t per = (size_t)E * d * ffn;
     const int nrange = seg_end - seg_begin;
-    // one position of the row list per thread up to 256 workgroups
-    const int build_grid = (int)(A <= 1024 ? 2 : (A > 255 * 1024 ? 256 : ceil_div64(A, 1024) + 1));
     int rc;
     // the table builder's turn; false: the call ends here
     auto tables = [&](const TableJob& job, int* rc_out) {
@@ -698,8 +686,7 @@ int grouped_ffn_call(int relu, const void* x_in, int64_t rows_in, const int32_t*
             return false;
         }
         if (stage == kFfnTablesBuilt) return true;
-        hipLaunchKernelGGL(build_tables_kernel, dim3(build_grid), dim3(1024), 0, st, seg_offsets, slot_expert, job);
-        *rc_out = check_launch();
+        *rc_out = launch_tables(A, seg_offsets, slot_expert, job, st);
         return *rc_out == MOE_OK;
     };
     // Forms of the first product's kernels, and how they find their rows: the streaming ones, with a handful of rows to an

@@ -204,3 +204,206 @@ def test_refusals_on_the_device():
         B.moe_combine_backward(x, y.float(), rows, w)
     with pytest.raises(B.MoeGpsError, match="invalid argument"):
         B.moe_combine_backward(x, y, rows, w, topk_idx=rows.view(4, 2), E=1)
+
+
+# ---------------------------------------------------------------------------
+# gradient of the grouped FFN
+# ---------------------------------------------------------------------------
+def ffn_case(rows_of_slot, slot_expert, E, k, d, ffn, dtype, relu, seed, x_scale=1.0):
+    """Random tensors for the given segments; the rows are a random permutation of the assignments."""
+    rng = np.random.default_rng(seed)
+    A = int(sum(rows_of_slot))
+    assert A % k == 0
+    seg = np.concatenate([[0], np.cumsum(rows_of_slot)]).astype(np.int32)
+    c = dict(E=E, k=k, d=d, ffn=ffn, dtype=dtype, relu=relu, seg=seg, slot_expert=np.asarray(slot_expert, np.int32),
+             assign=rng.permutation(A).astype(np.int32))
+    c["x"] = dev(rng.normal(size=(A // k, d)) * x_scale, dtype)
+    c["dy"] = dev(rng.normal(size=(A, d)) * 1e-2, dtype)
+    c["W1"] = dev(rng.normal(size=(E, d, ffn)) * d ** -0.5, dtype)
+    c["W3"] = None if relu else dev(rng.normal(size=(E, d, ffn)) * d ** -0.5, dtype)
+    c["W2"] = dev(rng.normal(size=(E, ffn, d)) * d ** -0.5, dtype)
+    return c
+
+
+def run_ffn(c, x=None, out=None, workspace=None):
+    packed = B.moe_pack_weights_relu(c["W1"], c["W2"]) if c["relu"] else B.moe_pack_weights(c["W1"], c["W3"], c["W2"])
+    back = B.moe_pack_weights_backward(c["W1"], c["W3"], c["W2"])
+    return B.moe_grouped_ffn_backward(c["x"] if x is None else x, dev_i32(c["assign"]), c["k"], c["dy"], dev_i32(c["seg"]),
+                                      dev_i32(c["slot_expert"]), packed, back, c["E"], c["ffn"], relu=c["relu"], out=out,
+                                      workspace=workspace)
+
+
+def ffn_reference(c, x):
+    """(values, worst-case errors) of dx_perm, dW1, dW3, dW2 in 64 bits.  A sum of n products in fp32 is off by n * 2^-24 of the sum
+    of their magnitudes at most; dh, h, da and db are rounded to the type once, results too; a, b and the exponential's and
+    reciprocal's few units (times |a|) reach h, da and db through the derivatives, all of them 1.1 at most."""
+    E, d, ffn, relu = c["E"], c["d"], c["ffn"], c["relu"]
+    u = UNIT[c["dtype"]]
+    gamma = lambda n: (n + 4) * U32
+    dy_all, token = host(c["dy"]), c["assign"] // c["k"]
+    W1, W2 = host(c["W1"]), host(c["W2"])
+    W3 = None if relu else host(c["W3"])
+    names = ("dx", "dW1", "dW3", "dW2")
+    shapes = dict(dx=dy_all.shape, dW1=W1.shape, dW3=W1.shape, dW2=W2.shape)
+    val, tol = {n: np.zeros(shapes[n]) for n in names}, {n: np.zeros(shapes[n]) for n in names}
+    for e in range(E):
+        r = np.concatenate([np.arange(c["seg"][s], c["seg"][s + 1]) for s in range(len(c["slot_expert"]))
+                            if c["slot_expert"][s] == e] or [np.zeros(0, int)]).astype(int)
+        n = len(r)
+        xe, dy = x[token[r]], dy_all[r]
+        a, dh = xe @ W1[e], dy @ W2[e].T
+        ta, th = gamma(d) * (abs(xe) @ abs(W1[e])), u * abs(dh) + (1 + u) * gamma(d) * (abs(dy) @ abs(W2[e]).T)
+        if relu:
+            h, da = np.maximum(a, 0), np.where(a > 0, dh, 0)
+            t_h = ta + u * abs(h)
+            t_da = np.where(a > 0, th, 0) + u * abs(da) + np.where(abs(a) <= ta, abs(dh) + th, 0)  # either side of 0
+            val["dx"][r], tol["dx"][r] = da @ W1[e].T, (t_da + gamma(ffn) * abs(da)) @ abs(W1[e]).T
+        else:
+            b = xe @ W3[e]
+            tb = gamma(d) * (abs(xe) @ abs(W3[e]))
+            s = 1 / (1 + np.exp(-a))
+            f = s + a * s * (1 - s)
+            ex = (np.abs(a) + 8) * 2.0 ** -22
+            h, da, db = a * s * b, dh * b * f, dh * a * s
+            t_h = abs(a * s) * tb + abs(b) * (1.1 * ta + ex * abs(a * s)) + u * abs(h)
+            t_db = abs(a * s) * th + (abs(dh) + th) * (1.1 * ta + ex * abs(a * s)) + u * abs(db)
+            t_da = abs(b * f) * th + (abs(dh) + th) * (abs(f) * tb + (abs(b) + tb) * (1.1 * ta + ex)) + u * abs(da)
+            val["dx"][r] = da @ W1[e].T + db @ W3[e].T
+            tol["dx"][r] = (t_da + gamma(2 * ffn) * abs(da)) @ abs(W1[e]).T + (t_db + gamma(2 * ffn) * abs(db)) @ abs(W3[e]).T
+            val["dW3"][e], tol["dW3"][e] = xe.T @ db, abs(xe).T @ (t_db + gamma(n) * abs(db))
+        val["dW1"][e], tol["dW1"][e] = xe.T @ da, abs(xe).T @ (t_da + gamma(n) * abs(da))
+        val["dW2"][e], tol["dW2"][e] = h.T @ dy, (t_h + gamma(n) * abs(h)).T @ abs(dy)
+    for n in names:
+        tol[n] += u * (abs(val[n]) + tol[n]) + 1e-38
+    return val, tol
+
+
+def check_ffn(c, got, x=None):
+    val, tol = ffn_reference(c, host(c["x"]) if x is None else x)
+    # the roundings of a long sum's terms are independent: the error's norm is that of two roundings and the result's own, each
+    # uniform within its half step, sqrt(3) / sqrt(3) of one
+    norm = UNIT[c["dtype"]] if c["dtype"] == "bf16" else 64 * U32
+    for name, t in zip(("dx", "dW1", "dW3", "dW2"), got):
+        if t is None:
+            continue
+        g = host(t)
+        err = np.abs(g - val[name])
+        assert np.all(err <= tol[name]), (name, float((err - tol[name]).max()), np.argwhere(err > tol[name])[:4])
+        size = np.linalg.norm(val[name])
+        if not c["relu"] or c["dtype"] == "bf16":
+            assert np.linalg.norm(g - val[name]) <= norm * size + 1e-30, (name, np.linalg.norm(g - val[name]) / max(size, 1e-300))
+
+
+SEGMENTS = {  # rows of the slots, their experts, E
+    "one_row": ([1], [0], 1),
+    "two_experts": ([3, 5], [1, 0], 2),
+    "empty_slots_and_experts": ([0, 7, 0, 1, 0], [2, 0, -1, 3, 2], 5),
+    "replicas": ([17, 33, 16, 30], [1, 0, 1, 0], 2),
+    "edges": ([31, 32, 33, 15, 64, 65], [0, 1, 2, 3, 4, 5], 6),
+    "tall": ([300, 2, 258], [0, 1, 2], 4),
+}
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("relu", [False, True])
+@pytest.mark.parametrize("segments", sorted(SEGMENTS))
+@pytest.mark.parametrize("d,ffn", [(64, 64), (128, 100), (320, 264)])
+def test_ffn_backward(dtype, relu, segments, d, ffn):
+    rows, experts, E = SEGMENTS[segments]
+    c = ffn_case(rows, experts, E, 1, d, ffn, dtype, relu, seed=len(rows) + d)
+    got = run_ffn(c)
+    check_ffn(c, got)
+    if relu:
+        assert got[2] is None
+    again = run_ffn(c)
+    assert all(a is None or torch.equal(a, b) for a, b in zip(got, again))
+
+
+@pytest.mark.parametrize("d,ffn", [(64, 1), (64, 7), (128, 65), (192, 130), (64, 520), (576, 66)])
+def test_ffn_backward_bf16_odd_widths(d, ffn):
+    """Hidden widths that are no multiple of eight (gradients stored value by value), of 64 or of a tile."""
+    c = ffn_case([9, 0, 40], [1, 2, 0], 3, 1, d, ffn, "bf16", False, seed=ffn)
+    check_ffn(c, run_ffn(c))
+    c = ffn_case([9, 0, 40], [1, 2, 0], 3, 1, d, ffn, "bf16", True, seed=ffn)
+    check_ffn(c, run_ffn(c))
+
+
+@pytest.mark.parametrize("d,ffn", [(4, 4), (12, 20), (132, 68)])
+def test_ffn_backward_f32_narrow(d, ffn):
+    for relu in (False, True):
+        c = ffn_case([5, 0, 70], [1, 2, 0], 3, 1, d, ffn, "f32", relu, seed=ffn)
+        check_ffn(c, run_ffn(c))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_ffn_backward_of_tokens_with_several_experts(dtype):
+    """k rows of a token, from the rows themselves and from a checkpoint of them."""
+    rng = np.random.default_rng(7)
+    k, T, E, d, ffn = 3, 150, 7, 256, 192
+    sizes = rng.multinomial(T * k, rng.dirichlet(np.ones(9)))
+    experts = [0, 1, 2, 3, 4, 5, 6, 2, 5]
+    c = ffn_case(sizes.tolist(), experts, E, k, d, ffn, dtype, False, seed=3)
+    check_ffn(c, run_ffn(c))
+    kept = B.moe_checkpoint_store(c["x"])
+    x = ck.load(kept[0].view(torch.uint8).cpu().numpy(), kept[1].cpu().numpy())
+    got = run_ffn(c, x=kept)
+    check_ffn(c, got, x)
+    # the rows that the checkpoint stands for are exact in the type: the same bits
+    plain = run_ffn(c, x=B.moe_checkpoint_load(*kept, DT[dtype]))
+    assert all(torch.equal(a, b) for a, b in zip(got, plain))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_ffn_backward_parts(dtype):
+    """Only dx, only the weights' gradients, nothing; outputs and workspace that held NaN; rows of no expert."""
+    rows, experts = [40, 5, 13], [0, -1, 1]
+    c = ffn_case(rows, experts, 3, 2, 128, 72, dtype, False, seed=11)
+    full = run_ffn(c)
+    nan = lambda t: torch.full_like(t, float("nan"))
+    dirty = tuple(nan(t) for t in full)
+    ws = torch.full((B.moe_grouped_ffn_backward_workspace_bytes(29, 2, 128, 72, 3, 3, B.dtype_code(c["dy"])),), 0xff,
+                    dtype=torch.uint8, device="cuda")
+    got = run_ffn(c, out=dirty, workspace=ws)
+    live = torch.ones(58, dtype=torch.bool, device="cuda")
+    live[40:45] = False
+    assert torch.equal(got[0][live], full[0][live]) and torch.isnan(got[0][~live]).all()
+    assert all(torch.equal(a, b) for a, b in zip(got[1:], full[1:]))
+    assert torch.all(got[1][2] == 0) and torch.all(got[3][2] == 0)
+    only = run_ffn(c, out=(nan(full[0]), None, None, None))
+    assert torch.equal(only[0][live], full[0][live])
+    only = run_ffn(c, out=(None, *[nan(t) for t in full[1:]]))
+    assert all(torch.equal(a, b) for a, b in zip(only[1:], full[1:]))
+    assert run_ffn(c, out=(None, None, None, None)) == (None, None, None, None)
+    with pytest.raises(B.MoeGpsError, match="invalid argument"):
+        run_ffn(c, out=(full[0], full[1], None, full[3]))
+    with pytest.raises(B.MoeGpsError, match="workspace too small"):
+        run_ffn(c, workspace=ws[:-256])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_ffn_backward_of_an_empty_batch(dtype):
+    c = ffn_case([0, 0], [0, 1], 2, 1, 64, 64, dtype, False, seed=1)
+    got = run_ffn(c, out=(c["dy"], *(torch.full_like(c[w], 3.0) for w in ("W1", "W3", "W2"))))
+    assert all(torch.all(t == 0) for t in got[1:])
+
+
+def test_ffn_backward_against_differences():
+    """fp32, in the direction of each gradient: a step that changes the loss by 2 eps |g|^2 (central difference of the library's own
+    forward pass, whose fp32 sums are off by about 1e-6 of the loss's terms)."""
+    c = ffn_case([20, 12, 31], [0, 1, 0], 2, 1, 64, 96, "f32", False, seed=5)
+    got = run_ffn(c)
+    x_perm = c["x"][torch.from_numpy(c["assign"].astype(np.int64)).cuda()]
+
+    def loss(**changed):
+        t = {**dict(x=x_perm, W1=c["W1"], W3=c["W3"], W2=c["W2"]), **changed}
+        packed = B.moe_pack_weights(t["W1"], t["W3"], t["W2"])
+        y = B.moe_grouped_ffn(t["x"], dev_i32(c["seg"]), dev_i32(c["slot_expert"]), packed, 2, 96)
+        return float((y.double() * c["dy"].double()).sum())
+
+    base = dict(x=x_perm, W1=c["W1"], W3=c["W3"], W2=c["W2"])
+    for name, g in zip(("x", "W1", "W3", "W2"), got):
+        n = float(g.double().norm())
+        step = 1e-2 * float(base[name].double().norm()) / n
+        up, down = (loss(**{name: base[name] + s * step * g}) for s in (1, -1))
+        # third derivatives: (1e-2)^2 relative at most a few times; rounding: 1e-6 of the terms, against a change of 1e-2 of them
+        assert abs((up - down) / (2 * step) - n * n) <= 2e-3 * n * n, name
