@@ -77,7 +77,7 @@ int moe_combine_backward(const void* dout, int dtype, int T, int d, int k, int E
  *   dx_perm    [T*k, d] dtype out, rows of segments whose slot holds no expert are not written; NULL: not wanted
  *   dW1, dW3 [E, d, ffn], dW2 [E, ffn, d] dtype out, written whole (zeros for experts without rows); NULL, all of them: not
  *              wanted.  dW3 is NULL with relu
- * bf16: sums in fp32; dh, h, da and db are rounded to bf16 as operands of the next products, results once.  The result does
+ * bf16: sums in fp32; h, da and db are rounded to bf16 as operands of the next products, results once.  The result does
  * not depend on the order in which parts of the launch run.  Outputs and workspace overlap nothing.
  * bf16 needs d % 64 == 0 and T*k*d < 2^31, f32 d % 4 == 0 and ffn % 4 == 0; limits otherwise as in the forward pass.
  * T = 0 writes zeros to the weight gradients.  Arguments are checked before the first launch.

@@ -5,14 +5,15 @@
 //     dx = da W1^T + db W3^T,  dW1 = x^T da,  dW3 = x^T db,  dW2 = h^T dy
 // and in the ReLU form h = max(a, 0), da = dh where a > 0, dx = da W1^T, dW1 = x^T da, dW2 = h^T dy.
 //
-// bf16: sums in fp32.  Rounded to bf16 on the way are dh, h, da and db, which are operands of further matrix products
-// (as h is in the forward pass): four half steps of 2^-8, each on its own term of a long sum.  Rows are worked on in the order of the
+// bf16: sums in fp32.  Rounded to bf16 on the way are h, da and db, which are operands of further matrix products
+// (as h is in the forward pass): a half step of 2^-8 each, on the terms of a long sum.  dh is not (with it rounded too, the
+// gradients' error grows by a fifth, and the bytes that halving it saves are 1 to 2 % of a call).  Rows are worked on in the order of the
 // forward pass's row list (by expert, replicas together):
 //   1. dh = dy W2^T             tiles of ffn_tiles.h, weights packed for it (moe_pack_weights_backward)
-//   2. a, b and from them and dh: h in the place of dh, da and db side by side in the packed order of the columns of a and b
+//   2. a, b and from them and dh: h, and da and db side by side in the packed order of the columns of a and b
 //                               tiles of ffn_tiles.h, the forward pass's packed weights
-//   3. dW1, dW3 and 4. dW2      ffn_weight_grad.h
-//   5. dx                       tiles of ffn_tiles.h, one sum over da's and db's columns
+//   3. dW1, dW3 and dW2         ffn_weight_grad.h
+//   4. dx                       tiles of ffn_tiles.h, one sum over da's and db's columns
 // fp32: three launches of plain LDS tiles (below), from the forward pass's packed weights alone.
 #include "ffn_device.h"
 #include "checkpoint.h"
@@ -28,9 +29,18 @@ template <int EPI>
 __global__ __launch_bounds__(512, 2) void hidden_grad_kernel(
     const bf16_t* __restrict__ X, int d, const bf16_t* __restrict__ P13, size_t b_stride, bf16_t* __restrict__ dab,
     const MTile* __restrict__ mtiles, const int32_t* __restrict__ counts, int32_t* __restrict__ queues, int N,
-    bool past_caches, RowMap rm, bf16_t* hidden) {
+    bool past_caches, RowMap rm, const float* __restrict__ dhidden, bf16_t* __restrict__ hidden) {
     tile_product<EPI, kAlone>(X, d, P13, b_stride, dab, N, mtiles, counts, queues, N, d, kTileGroup, past_caches, rm, nullptr,
-                              RowCopy{}, nullptr, hidden);
+                              RowCopy{}, nullptr, dhidden, hidden);
+}
+
+// dh = dy W2^T, in fp32.
+__global__ __launch_bounds__(512, 2) void dhidden_kernel(
+    const bf16_t* __restrict__ dy, int d, const bf16_t* __restrict__ P2, size_t b_stride, float* __restrict__ dhidden,
+    const MTile* __restrict__ mtiles, const int32_t* __restrict__ counts, int32_t* __restrict__ queues, int N,
+    bool past_caches, RowMap rm) {
+    tile_product<kEpiFloat, kAlone>(dy, d, P2, b_stride, nullptr, N, mtiles, counts, queues, N, d, kTileGroup, past_caches, rm,
+                                    dhidden, RowCopy{}, nullptr);
 }
 
 // ---------------------------------------------------------------------------
@@ -256,13 +266,14 @@ __global__ __launch_bounds__(256) void f32_grads_kernel(F32Backward p) {
 // ---------------------------------------------------------------------------
 struct BackwardWs {
     void* x;             // [T, d] rows of x, from a checkpoint
-    void *hidden, *dab;  // [A, fp] dh, then h; [A, n1 * fp] da (and db)
+    float* dhidden;      // [A, fp] dh (bf16)
+    void *hidden, *dab;  // [A, fp] h; [A, n1 * fp] da (and db)
     int32_t *rows, *tokens, *bases;
     MTile *tiles1, *tiles2;
     int32_t *counts, *queues;
     int capacity;
 };
-constexpr int kBackwardQueues = 3 * 8;
+constexpr int kBackwardQueues = 5 * 8;  // claim counters of the three products and of the weight gradients
 
 static size_t backward_layout(int64_t T, int k, int d, int ffn, int E, int nseg, int dtype, int relu, char* base,
                               BackwardWs* ws) {
@@ -277,6 +288,7 @@ static size_t backward_layout(int64_t T, int k, int d, int ffn, int E, int nseg,
     BackwardWs w;
     w.capacity = (int)(ceil_div64(A1, kMinBM) + nseg);
     w.x = take((size_t)T1 * d * size);
+    w.dhidden = (float*)take(dtype == MOE_DTYPE_BF16 ? (size_t)A1 * fp * sizeof(float) : 0);
     w.hidden = take((size_t)A1 * fp * size);
     w.dab = take((size_t)A1 * fp * size * (relu ? 1 : 2));
     w.rows = (int32_t*)take((size_t)A1 * sizeof(int32_t));
@@ -298,13 +310,13 @@ static bool backward_in_range(int T, int k, int d, int ffn, int E, int nseg, int
 // workgroups of a launch that goes round its tiles
 static unsigned tile_grid(int64_t tiles) { return (unsigned)(tiles < 1 ? 1 : tiles < (1 << 20) ? tiles : 1 << 20); }
 
-template <bool PAIR, bool P_LISTED>
-static int launch_weight_grad(const WeightGrad& w, hipStream_t st) {
-    const auto kern = weight_grad_kernel<PAIR, P_LISTED>;
+template <bool PAIR>
+static int launch_weight_grads(const WeightGrad& w13, const WeightGrad& w2, const int32_t* bases, int32_t* queues, int E,
+                               hipStream_t st) {
+    const auto kern = weight_grads_kernel<PAIR>;
     static std::atomic<unsigned long long> raised{0};
-    if (const int rc = raise_lds((const void*)kern, kGradLds, raised); rc != MOE_OK) return rc;
-    const int64_t tiles = (int64_t)w.E * ceil_div(w.M, kGradTile) * ceil_div(w.N, kGradTile);
-    hipLaunchKernelGGL(kern, dim3(tile_grid(tiles)), dim3(512), kGradLds, st, w);
+    if (const int rc = raise_lds((const void*)kern, grad_lds(MOE_MAX_EXPERTS), raised); rc != MOE_OK) return rc;
+    hipLaunchKernelGGL(kern, dim3(kGemmGrid), dim3(512), grad_lds(E), st, w13, w2, bases, queues, E);
     return check_launch();
 }
 
@@ -315,7 +327,16 @@ static int launch_hidden_grad(const bf16_t* x, int d, const bf16_t* p13, size_t 
     static std::atomic<unsigned long long> raised{0};
     if (const int rc = raise_lds((const void*)kern, kTileLds<EPI>, raised); rc != MOE_OK) return rc;
     hipLaunchKernelGGL(kern, dim3(kGemmGrid), dim3(512), kTileLds<EPI>, st, x, d, p13, stride, (bf16_t*)ws.dab, ws.tiles1,
-                       ws.counts, ws.queues + 8, N, past_caches(E, stride), rm, (bf16_t*)ws.hidden);
+                       ws.counts, ws.queues + 8, N, past_caches(E, stride), rm, ws.dhidden, (bf16_t*)ws.hidden);
+    return check_launch();
+}
+
+static int launch_dhidden(const bf16_t* dy, int d, const bf16_t* p2, size_t stride, int E, const BackwardWs& ws, int N,
+                          const RowMap& rm, hipStream_t st) {
+    static std::atomic<unsigned long long> raised{0};
+    if (const int rc = raise_lds((const void*)dhidden_kernel, kTileLds<kEpiFloat>, raised); rc != MOE_OK) return rc;
+    hipLaunchKernelGGL(dhidden_kernel, dim3(kGemmGrid), dim3(512), kTileLds<kEpiFloat>, st, dy, d, p2, stride, ws.dhidden,
+                       ws.tiles1, ws.counts, ws.queues, N, past_caches(E, stride), rm);
     return check_launch();
 }
 
@@ -349,18 +370,18 @@ static int backward_bf16(const moe_ffn_backward_args& a, const bf16_t* x, const 
     int rc = MOE_OK;
     const RowMap by_row{ws.rows, nullptr, 1, nullptr, nullptr, nullptr}, by_token{ws.tokens, nullptr, 1, nullptr, nullptr, nullptr};
     if (a.T > 0) {
-        rc = launch_product((const bf16_t*)a.dy_perm, d, back2, packed_back2(d, fp), a.E, hidden, fp, ws.tiles1, ws.counts, ws.queues,
-                            fp, d, by_row, st);
+        rc = launch_dhidden((const bf16_t*)a.dy_perm, d, back2, packed_back2(d, fp), a.E, ws, fp, by_row, st);
         if (rc == MOE_OK)
             rc = a.relu ? launch_hidden_grad<kEpiReluGrad>(x, d, p13, packed_elems1(1, d, fp), a.E, ws, fp, by_token, st)
                         : launch_hidden_grad<kEpiSwigluGrad>(x, d, p13, packed_elems1(2, d, fp), a.E, ws, 2 * fp, by_token, st);
     }
     if (rc == MOE_OK && a.dW1) {
+        const WeightGrad w13{x, dab, ws.tokens, d, n1 * fp, {(bf16_t*)a.dW1, (bf16_t*)a.dW3}, d, n1 * fp, d, a.ffn};
+        const WeightGrad w2{hidden, (const bf16_t*)a.dy_perm, ws.rows, fp, d, {(bf16_t*)a.dW2, nullptr}, fp, d, a.ffn, d};
         const int32_t* bases = a.T > 0 ? ws.bases : nullptr;
-        const WeightGrad w13{x, dab, ws.tokens, d, n1 * fp, bases, {(bf16_t*)a.dW1, (bf16_t*)a.dW3}, d, n1 * fp, d, a.ffn, a.E};
-        const WeightGrad w2{hidden, (const bf16_t*)a.dy_perm, ws.rows, fp, d, bases, {(bf16_t*)a.dW2, nullptr}, fp, d, a.ffn, d, a.E};
-        rc = a.relu ? launch_weight_grad<false, true>(w13, st) : launch_weight_grad<true, true>(w13, st);
-        if (rc == MOE_OK) rc = launch_weight_grad<false, false>(w2, st);
+        int32_t* queues = a.T > 0 ? ws.queues + 24 : nullptr;
+        rc = a.relu ? launch_weight_grads<false>(w13, w2, bases, queues, a.E, st)
+                    : launch_weight_grads<true>(w13, w2, bases, queues, a.E, st);
     }
     if (rc == MOE_OK && a.T > 0 && a.dx_perm) {
         const RowMap to_row{nullptr, nullptr, 1, ws.rows, nullptr, nullptr};

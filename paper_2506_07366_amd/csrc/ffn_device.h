@@ -108,9 +108,9 @@ __device__ __forceinline__ float silu_f(float g) { return g * __builtin_amdgcn_r
 // EPI selects what happens to the accumulators before they are stored: kEpiNone (plain
 // product, optionally scaled per row), kEpiSwiglu (silu(gate) * up on interleaved column
 // pairs, half as many output columns), kEpiRelu (max(., 0)); in the backward pass (ffn_backward.hip)
-// kEpiSwigluGrad and kEpiReluGrad (the hidden activation and the gradients of what it is made of, from the
-// gradient of the hidden activation).
-constexpr int kEpiNone = 0, kEpiSwiglu = 1, kEpiRelu = 2, kEpiSwigluGrad = 3, kEpiReluGrad = 4;
+// kEpiFloat (plain product in place, not rounded) and kEpiSwigluGrad and kEpiReluGrad (the hidden activation and the
+// gradients of what it is made of, from the gradient of the hidden activation).
+constexpr int kEpiNone = 0, kEpiSwiglu = 1, kEpiRelu = 2, kEpiSwigluGrad = 3, kEpiReluGrad = 4, kEpiFloat = 5;
 // the first products of the forward pass take a share of the row copy along
 constexpr bool epi_copies(int epi) { return epi == kEpiSwiglu || epi == kEpiRelu; }
 

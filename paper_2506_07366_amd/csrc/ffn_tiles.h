@@ -77,11 +77,12 @@ __device__ __forceinline__ void tile_product(
     bf16_t* C, int ldc,                              // output [rows, SWIGLU ? N/2 : N]
     const MTile* __restrict__ mtiles, const int32_t* __restrict__ counts, int32_t* __restrict__ queues,
     int N, int K, int group_n, bool past_caches, RowMap rm,
-    float* __restrict__ partials,  // [slab][kPartRows][N] fp32 sums of entries that cover part of K (plain product, a launch of its own)
+    float* __restrict__ partials,  // [slab][kPartRows][N] fp32 sums of entries that cover part of K (plain product, a launch of its own);
+                                   //   kEpiFloat: the output [rows, N]
     RowCopy copy,                  // first product: rows to be copied besides, a share of them with every tile
     int32_t* left,                 // [E] what the second product waits for, see above (LINK)
-    bf16_t* hidden = nullptr) {    // backward pass: [rows, SWIGLU ? N/2 : N] gradient of the hidden activation in, the
-                                   //   hidden activation out
+    const float* dhidden = nullptr,  // backward pass: [rows, SWIGLU ? N/2 : N] gradient of the hidden activation,
+    bf16_t* hidden = nullptr) {      //   and out the hidden activation
     constexpr bool SWIGLU = EPI == kEpiSwiglu || EPI == kEpiSwigluGrad;
     constexpr int BN = kPackN, BK = kPackK, NW = 8;
     constexpr int ROW_BYTES = BK * 2;      // of an activation row in a stage
@@ -435,18 +436,17 @@ __device__ __forceinline__ void tile_product(
         if constexpr (EPI == kEpiSwigluGrad) {
             // With a = x W1, b = x W3, s = 1 / (1 + exp(-a)) and the gradient dh of h = a s b:
             //     db = dh a s,   da = dh b s (1 + a (1 - s)),
-            // stored side by side in the packed columns of a and b.  h goes where dh was: a wavefront has read all it needs of
-            // its columns before it writes to them (and all at once: one memory round trip).
+            // stored side by side in the packed columns of a and b.  dh is fetched for all rows at once: one memory round trip.
             const int f0 = n0 / 2 + (wave >> 1) * 32 + (wave & 1) * 16, c0 = n0 + (wave >> 1) * 64 + (wave & 1) * 16;
             const int ldh = N / 2;
-            uint2 raw[TM_MAX];
+            f32x4 dh[TM_MAX];
 #pragma unroll
             for (int i = 0; i < TM_MAX; ++i) {
                 const int row = i * 16 + l16e;
-                raw[i] = uint2{0u, 0u};
+                dh[i] = f32x4{0.f, 0.f, 0.f, 0.f};
                 if ((i & ~1) * 16 < mt.rows && f0 < ldh)
-                    raw[i] = *(const uint2*)(hidden + (size_t)(mt.list0 + (row < mt.rows ? row : mt.rows - 1)) * ldh + f0 +
-                                             g16e * 4);
+                    dh[i] = *(const f32x4*)(dhidden + (size_t)(mt.list0 + (row < mt.rows ? row : mt.rows - 1)) * ldh + f0 +
+                                            g16e * 4);
             }
 #pragma unroll
             for (int i = 0; i < TM_MAX; i += 2) {
@@ -456,14 +456,12 @@ __device__ __forceinline__ void tile_product(
                     for (int q = 0; q < 2; ++q)
 #pragma unroll
                         for (int c = 0; c < 4; ++c) {
-                            const unsigned word = c < 2 ? raw[i + q].x : raw[i + q].y;
-                            const float dh = __builtin_bit_cast(float, c & 1 ? word & 0xffff0000u : word << 16);
                             const float a = acc[i + q][0][c], b = acc[i + q][1][c];
                             const float s = __builtin_amdgcn_rcpf(1.0f + __expf(-a));
                             const float as = a * s;
                             h[q][c] = as * b;
-                            db[q][c] = dh * as;
-                            da[q][c] = dh * b * fmaf(as, 1.0f - s, s);
+                            db[q][c] = dh[i + q][c] * as;
+                            da[q][c] = dh[i + q][c] * b * fmaf(as, 1.0f - s, s);
                         }
                     const int row = (i + (g16e >> 1)) * 16 + l16e;
                     const bool on = row < mt.rows && f0 < ldh;
@@ -474,34 +472,37 @@ __device__ __forceinline__ void tile_product(
                 }
             }
         } else if constexpr (EPI == kEpiReluGrad) {
-            // a = x W1, h = max(a, 0), da = dh where a > 0 and 0 elsewhere (also at 0); h goes where dh was, as above.
+            // a = x W1, h = max(a, 0), da = dh where a > 0 and 0 elsewhere (also at 0); dh of eight row groups at a time.
             const int col0 = n0 + wave * 32;
-            uint2 raw[TM_MAX][2];
 #pragma unroll
-            for (int i = 0; i < TM_MAX; ++i)
+            for (int i0 = 0; i0 < TM_MAX; i0 += 8) {
+                if (i0 * 16 >= mt.rows) continue;
+                f32x4 dh[8][2];
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const int row = i * 16 + l16e;
-                    raw[i][j] = uint2{0u, 0u};
-                    if (i * 16 < mt.rows && col0 < N)
-                        raw[i][j] = *(const uint2*)(hidden + (size_t)(mt.list0 + (row < mt.rows ? row : mt.rows - 1)) * N +
-                                                    col0 + j * 16 + g16e * 4);
-                }
+                for (int i = 0; i < 8; ++i)
 #pragma unroll
-            for (int i = 0; i < TM_MAX; ++i) {
-                if (i * 16 < mt.rows) {
+                    for (int j = 0; j < 2; ++j) {
+                        const int row = (i0 + i) * 16 + l16e;
+                        dh[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+                        if ((i0 + i) * 16 < mt.rows && col0 < N)
+                            dh[i][j] = *(const f32x4*)(dhidden + (size_t)(mt.list0 + (row < mt.rows ? row : mt.rows - 1)) * N +
+                                                       col0 + j * 16 + g16e * 4);
+                    }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    if ((i0 + i) * 16 >= mt.rows) continue;
                     float h[2][4], da[2][4];
 #pragma unroll
                     for (int j = 0; j < 2; ++j)
 #pragma unroll
                         for (int c = 0; c < 4; ++c) {
-                            const unsigned word = c < 2 ? raw[i][j].x : raw[i][j].y;
-                            const float a = acc[i][j][c];
+                            const float a = acc[i0 + i][j][c];
                             h[j][c] = fmaxf(a, 0.f);
-                            da[j][c] = a > 0.f ? __builtin_bit_cast(float, c & 1 ? word & 0xffff0000u : word << 16) : 0.f;
+                            da[j][c] = a > 0.f ? dh[i][j][c] : 0.f;
                         }
-                    const bool on = i * 16 + l16e < mt.rows && col0 < N;
-                    const size_t at = (size_t)(mt.list0 + i * 16 + l16e);
+                    const int row = (i0 + i) * 16 + l16e;
+                    const bool on = row < mt.rows && col0 < N;
+                    const size_t at = (size_t)(mt.list0 + row);
                     store_pair(h[0], h[1], hidden + at * N + col0 + g16e * 8, on);
                     store_pair(da[0], da[1], C + at * ldc + col0 + g16e * 8, on);
                 }
@@ -525,7 +526,8 @@ __device__ __forceinline__ void tile_product(
             float* slab = nullptr;
             if constexpr (EPI == kEpiNone && LINK == kAlone)
                 if (mt.part >= 0) slab = partials + (size_t)mt.part * kPartRows * N;
-            if (slab) {
+            if constexpr (EPI == kEpiFloat) slab = partials + (size_t)mt.list0 * N;
+            if (EPI == kEpiFloat || slab) {
 #pragma unroll
                 for (int i = 0; i < TM_MAX; ++i) {
                     const int row = i * 16 + l16e;

@@ -7,49 +7,121 @@
 // order of the 32 rows will do as long as both operands have the same, so a lane takes rows 4 g .. 4 g + 3 and 16 + 4 g ..
 // (g the quarter of the wavefront), and a half wavefront reads eight different rows at a time; piece (32 bytes) c of
 // row r stands at c ^ (r & 7), which puts these on eight different groups of banks.
+//
+// A workgroup of eight wavefronts makes a tile of 256 x 256, 128 columns of Q by 64 of P each.  Four steps of 32 rows have room in
+// LDS, three are under way; the rows of the listed operand are looked up four steps ahead of its loads.  A step is eight
+// fragments of Q against four of P; the hand-over to the next step stands two fragments before the end, so that its first
+// reads land under what is left to multiply.
 #pragma once
 
 struct WeightGrad {
     const bf16_t *p, *q;
     const int32_t* rows;     // of the listed operand: row of every list position
     int ldp, ldq;            // row lengths, both multiples of 64
-    const int32_t* bases;    // [E + 1] first list position of an expert; null: there are no rows
     bf16_t* out[2];          // [E][m_out][n_out]; packed pairs of columns: the first and the second matrix
     int M, N;                // columns of p and of q
     int m_out, n_out;
-    int E;
 };
 
 constexpr int kGradRows = 32, kGradTile = 256, kGradStages = 4;
 constexpr int kGradPanel = kGradRows * kGradTile * 2;                     // bytes of one operand in a stage
-constexpr size_t kGradLds = (size_t)2 * kGradStages * kGradPanel;
+constexpr int kGradNextAt = 2 * kGradStages * kGradPanel;                 // number of the next tile, behind the stages
+constexpr int kGradOrderAt = kGradNextAt + 16;                            // the experts, most rows first
+constexpr size_t grad_lds(int E) { return (size_t)kGradOrderAt + (size_t)E * sizeof(int32_t); }
 
 typedef __attribute__((__vector_size__(4 * sizeof(short)))) short s16x4;
 
+// Four rows of a column of a panel to every lane; see lds_read_b128 for when the result may be touched.
+template <int OFF>
+__device__ __forceinline__ void lds_read_tr(s16x4& dst, unsigned addr) {
+    asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(dst) : "v"(addr), "n"(OFF) : "memory");
+}
+
+struct GradFrag {  // 16 columns x 32 rows
+    s16x4 lo, hi;
+};
+__device__ __forceinline__ void landed(GradFrag& f) { asm volatile("" : "+v"(f.lo), "+v"(f.hi)); }
+__device__ __forceinline__ bf16x8 whole(const GradFrag& f) {
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(f.lo, f.hi, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+// A word of LDS, the same for the whole wavefront.  (As an ordinary read it would be taken to depend on every load into LDS under
+// way, and with those wait for the stores of the tile before.)
+__device__ __forceinline__ int lds_uniform(unsigned addr) {
+    int v;
+    asm volatile("ds_read_b32 %0, %1\n\ts_waitcnt lgkmcnt(0)" : "=v"(v) : "v"(addr) : "memory");
+    return __builtin_amdgcn_readfirstlane(v);
+}
+
+// The experts in LDS, those with most rows first (equal ones by number): big tiles at the end of a launch would be waited for.
+__device__ __forceinline__ void order_experts(int* order, int* count, const int32_t* bases, int E) {
+    for (int e = threadIdx.x; e < E; e += blockDim.x) count[e] = bases[e + 1] - bases[e];
+    __syncthreads();
+    for (int e = threadIdx.x; e < E; e += blockDim.x) {
+        const int mine = count[e];
+        int at = 0;
+        for (int o = 0; o < E; ++o) at += count[o] > mine || (count[o] == mine && o < e) ? 1 : 0;
+        order[at] = e;
+    }
+    __syncthreads();
+}
+
 // PAIR: columns of q are packed pairs in blocks of 32 (of one matrix, then of the other).  P_LISTED: the rows of p go through the
-// list, those of q are in place; else the reverse.
+// list, those of q are in place; else the reverse.  bases, queues null: there are no rows, and the tiles are dealt out evenly.
 template <bool PAIR, bool P_LISTED>
-__global__ __launch_bounds__(512, 2) void weight_grad_kernel(WeightGrad w) {
-    extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+__device__ __forceinline__ void weight_grad(const WeightGrad& w, const int32_t* bases, int32_t* queues, int E,
+                                            unsigned char* smem) {
     const int tid = threadIdx.x;
     const int lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int l16 = lane & 15, g16 = lane >> 4;
     const int wn = wave >> 2, wm = wave & 3;  // 128 columns of q by 64 of p each
     const int m_tiles = ceil_div(w.M, kGradTile), n_tiles = ceil_div(w.N, kGradTile);
-    const int64_t total = (int64_t)w.E * m_tiles * n_tiles;
+    const int per_expert = m_tiles * n_tiles;
+    const int64_t total = (int64_t)E * per_expert;
     const unsigned lds_base = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)smem;
+    volatile __attribute__((address_space(3))) int& next_tile =
+        *(volatile __attribute__((address_space(3))) int*)(__attribute__((address_space(3))) unsigned char*)(smem + kGradNextAt);
 
-    for (int64_t tile = blockIdx.x; tile < total; tile += gridDim.x) {
-        const int e = (int)(tile / (m_tiles * n_tiles));
-        const int in_e = (int)(tile - (int64_t)e * (m_tiles * n_tiles));
-        const int n0 = (in_e % n_tiles) * kGradTile, m0 = (in_e / n_tiles) * kGradTile;
-        const int first = w.bases ? w.bases[e] : 0, last = w.bases ? w.bases[e + 1] : 0;
+    // Tiles are claimed like those of ffn_tiles.h: runs of 32 consecutive ones go to the XCDs in turn, and the workgroups of an
+    // XCD, which share its L2, take the tiles of its runs one by one from a counter; one whose XCD has run dry goes on with
+    // the next XCD's.  The first claim of a workgroup is made in advance.
+    constexpr int run = kGemmGrid / 8;
+    int counter = blockIdx.x & 7, dry = 0;
+    int64_t mine = blockIdx.x;  // without counters
+    auto claimed = [&](int i) {  // tile of claim i of the counter, claiming on where it has run out; -1: no tile is left
+        for (;;) {
+            const int64_t t = ((int64_t)counter + 8 * (int64_t)(i / run)) * run + i % run;
+            if (t < total) return t;
+            if (++dry == 8) return (int64_t)-1;
+            counter = (counter + 1) & 7;
+            i = 0;
+            if (lane == 0) i = atomicAdd(&queues[counter], 1);
+            i = __builtin_amdgcn_readfirstlane(i);
+        }
+    };
+    // (a tile number fits: the gradients of more than 2^31 tiles would be 2^48 bytes)
+    if (wave == 0) next_tile = queues ? (int)claimed((int)(blockIdx.x >> 3)) : mine < total ? (int)mine : -1;
+
+    for (;;) {
+        lds_wait<0>();
+        __builtin_amdgcn_s_barrier();  // also: every wavefront has read the previous tile's stages
+        const int tile = lds_uniform(lds_base + kGradNextAt);
+        if (tile < 0) break;
+        int ahead = 0;  // the claim for the tile after this one, looked at behind the sum
+        if (queues && wave == 0 && lane == 0 && dry < 8) ahead = atomicAdd(&queues[counter], 1);
+        const int nth = tile / per_expert, in_e = tile - nth * per_expert;
+        const int e = bases ? lds_uniform(lds_base + kGradOrderAt + (unsigned)nth * 4u) : nth;
+        // four tiles side by side along n, down all of m, and so on
+        const int group = in_e / (m_tiles * kTileGroup), in_g = in_e - group * (m_tiles * kTileGroup);
+        const int gw = n_tiles - group * kTileGroup < kTileGroup ? n_tiles - group * kTileGroup : kTileGroup;
+        const int n0 = (group * kTileGroup + in_g % gw) * kGradTile, m0 = in_g / gw * kGradTile;
+        const int first = bases ? bases[e] : 0, last = bases ? bases[e + 1] : 0;
         const int KT = ceil_div(last - first, kGradRows);
 
-        // Loads: instruction i of a wavefront brings rows 2 (wave + 8 i) and + 1 of the step, 512 bytes each
-        const int row_of[2] = {2 * wave + (lane >> 5), 2 * (wave + 8) + (lane >> 5)};
-        const int piece = (lane & 31) ^ ((row_of[0] & 7) << 1);  // (the same for both rows, 16 apart)
+        // Loads: instruction i of a wavefront brings rows 2 (wave + 8 i) and + 1 of the step, 512 bytes each.
+        const int lane_p = opaque(lane);
+        const int row0 = 2 * wave + (lane_p >> 5);
+        const int piece = (lane_p & 31) ^ ((row0 & 7) << 1);  // (the same for both rows, 16 apart)
         constexpr unsigned kRange = 0xffffff80u, kPast = 0xfffffff0u;
         const unsigned colp = m0 + piece * 8 < w.M ? (unsigned)(m0 + piece * 8) * 2 : kPast;
         const unsigned colq = n0 + piece * 8 < w.N ? (unsigned)(n0 + piece * 8) * 2 : kPast;
@@ -60,80 +132,140 @@ __global__ __launch_bounds__(512, 2) void weight_grad_kernel(WeightGrad w) {
         const auto l_rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)listed, 0, (int)kRange, 0x00027000);
         unsigned off_i[2];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) off_i[i] = col_i == kPast ? kPast : (unsigned)row_of[i] * (unsigned)ld_i * 2u + col_i;
-        auto fetch_rows = [&](int kt, int (&r)[2]) {
+        for (int i = 0; i < 2; ++i)
+            off_i[i] = col_i == kPast ? kPast : (unsigned)(row0 + 16 * i) * (unsigned)ld_i * 2u + col_i;
+        int ids[4][2], ids_next[4][2];  // rows of the listed operand that the loads of four steps want, and of the next four
+        auto look_up = [&](int kt, int (&r)[2]) {
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const int p = first + kt * kGradRows + row_of[i];
+                const int p = first + kt * kGradRows + row0 + 16 * i;
                 r[i] = w.rows[p < last ? p : last - 1];
             }
         };
-        auto load = [&](int kt, int stage, const int (&r)[2]) {
-            unsigned char* to_p = smem + stage * kGradPanel;
-            unsigned char* to_q = smem + (kGradStages + stage) * kGradPanel;
+        auto load = [&](int kt, auto St, const int (&r)[2]) {
+            constexpr int stage = decltype(St)::value;
             const int p0 = first + kt * kGradRows;
             const int left = last - p0;  // rows from here on; past them both operands are zeros
             // in place: a descriptor of the rows that are left (none: an empty one)
             const unsigned n = left <= 0 ? 0u : (unsigned)(left < kGradRows ? left : kGradRows) * (unsigned)ld_i * 2u;
             const auto i_rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)(placed + (size_t)p0 * ld_i), 0, (int)n, 0x00027000);
+            unsigned char* to_l = smem + (P_LISTED ? stage : kGradStages + stage) * kGradPanel + wave * 1024;
+            unsigned char* to_i = smem + (P_LISTED ? kGradStages + stage : stage) * kGradPanel + wave * 1024;
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const unsigned off = row_of[i] < left && col_l != kPast ? (unsigned)r[i] * (unsigned)ld_l * 2u + col_l : kPast;
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(
-                    l_rsrc, (__attribute__((address_space(3))) void*)((P_LISTED ? to_p : to_q) + (wave + 8 * i) * 1024), 16, off,
-                    0, 0, 0);
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(
-                    i_rsrc, (__attribute__((address_space(3))) void*)((P_LISTED ? to_q : to_p) + (wave + 8 * i) * 1024), 16,
-                    off_i[i], 0, 0, 0);
+                const unsigned off = row0 + 16 * i < left && col_l != kPast ? (unsigned)r[i] * (unsigned)ld_l * 2u + col_l : kPast;
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(l_rsrc, (__attribute__((address_space(3))) void*)(to_l + 8192 * i), 16,
+                                                         off, 0, 0, 0);
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(i_rsrc, (__attribute__((address_space(3))) void*)(to_i + 8192 * i), 16,
+                                                         off_i[i], 0, 0, 0);
             }
         };
 
         f32x4 acc[8][4];
+        if (KT > 0) {
+            static_for<3>([&](auto U) { look_up(decltype(U)::value, ids_next[decltype(U)::value]); });
+            static_for<4>([&](auto U) { look_up(3 + decltype(U)::value, ids[decltype(U)::value]); });
+            static_for<3>([&](auto U) { load(decltype(U)::value, U, ids_next[decltype(U)::value]); });
+        }
 #pragma unroll
         for (int i = 0; i < 8; ++i)
 #pragma unroll
             for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
         // where the lane reads 16-column group c (of the 8 that share a swizzle) of rows 4 g16 + (l16 >> 2)
+        const int l16 = lane_p & 15, g16 = lane_p >> 4;
         const int rr = 4 * g16 + (l16 >> 2);
         const unsigned at = lds_base + (unsigned)(rr * 512 + (l16 & 3) * 8);
         unsigned q_at[8], p_at[4];
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            q_at[i] = at + kGradStages * kGradPanel + wn * 256 + ((i ^ (rr & 7)) * 32);
+        for (int i = 0; i < 8; ++i) q_at[i] = at + kGradStages * kGradPanel + wn * 256 + ((i ^ (rr & 7)) * 32);
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            p_at[j] = at + (wm >> 1) * 256 + ((((wm & 1) * 4 + j) ^ (rr & 7)) * 32);
+        for (int j = 0; j < 4; ++j) p_at[j] = at + (wm >> 1) * 256 + ((((wm & 1) * 4 + j) ^ (rr & 7)) * 32);
 
-        for (int kt = 0; kt < KT; ++kt) {
-            int r[2];
-            fetch_rows(kt, r);
-            load(kt, 0, r);
-            __syncthreads();
-            auto frag = [&](unsigned a) {
-                const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(size_t)a);
-                const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(size_t)(a + 16 * 512));
-                return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        if (KT > 0) {
+            GradFrag pf[2][4], qf[4];  // of q: fragment f in qf[f % 4]
+            auto read = [&](GradFrag& f, unsigned addr, auto St) {
+                constexpr int off = decltype(St)::value * kGradPanel;
+                lds_read_tr<off>(f.lo, addr);
+                lds_read_tr<off + 16 * 512>(f.hi, addr);
             };
-            bf16x8 qf[8], pf[4];
+            constexpr int kLoads = 4, kRows = 8;  // of a wavefront: a step's share of both panels; rows looked up in four steps
+            wait_vmcnt<2 * kLoads>();             // step 0 has landed
+            __builtin_amdgcn_s_barrier();
+            static_for<4>([&](auto J) { read(pf[0][decltype(J)::value], p_at[decltype(J)::value], std::integral_constant<int, 0>{}); });
+            static_for<4>([&](auto I) { read(qf[decltype(I)::value], q_at[decltype(I)::value], std::integral_constant<int, 0>{}); });
+            // step kt in stage U; 12 fragments of two reads each, in the order p0 .. p3, q0 .. q7.  MORE: one of four steps behind which
+            // others come (behind the others nobody wants the rows that step 0 would look up)
+            auto body = [&](int kt, auto U, auto more_tag) {
+                constexpr bool MORE = decltype(more_tag)::value;
+                constexpr int u = decltype(U)::value;
+                constexpr std::integral_constant<int, (u + 1) % 4> next{};
+                constexpr std::integral_constant<int, (u + 3) % 4> far{};
+                static_for<8>([&](auto F) {
+                    constexpr int f = decltype(F)::value;
+                    if constexpr (f == 6) {
+                        lds_wait<0>();                  // all reads of this step
+                        // step kt + 1 has landed: newer are steps kt + 2 and kt + 3, and rows looked up in step 0 of these four
+                        wait_vmcnt<2 * kLoads + (MORE && u < 3 ? kRows : 0)>();
+                        __builtin_amdgcn_s_barrier();
+                        static_for<4>([&](auto J) { read(pf[(u + 1) & 1][decltype(J)::value], p_at[decltype(J)::value], next); });
+                        static_for<2>([&](auto I) { read(qf[decltype(I)::value], q_at[decltype(I)::value], next); });
+                    } else if constexpr (f < 6) {
+                        lds_wait<(f <= 4 ? 6 : 4)>();   // fragment f has landed; newer are three (at f = 5 two) of q
+                    }
+                    if constexpr (f == 0) static_for<4>([&](auto J) { landed(pf[u & 1][decltype(J)::value]); });
+                    landed(qf[f % 4]);
+                    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) pf[j] = frag(p_at[j]);
+                    for (int j = 0; j < 4; ++j)
+                        acc[f][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(whole(qf[f % 4]), whole(pf[u & 1][j]), acc[f][j], 0, 0, 0);
+                    __builtin_amdgcn_sched_barrier(0);
+                    if constexpr (f < 4) read(qf[f], q_at[f + 4], U);
+                    else if constexpr (f >= 6) read(qf[f - 4], q_at[f - 4], next);
+                    // stage far was read a step ago; the barrier at that step's end says so for every wavefront
+                    if constexpr (f == 1) load(kt + 3, far, ids[u]);
+                    if constexpr (MORE && f == 2 && u == 0) static_for<4>([&](auto V) { look_up(kt + 7 + decltype(V)::value, ids_next[decltype(V)::value]); });
+                    __builtin_amdgcn_sched_barrier(0);
+                });
+            };
+            int kt = 0;
+            for (; kt + 4 < KT; kt += 4) {
+                static_for<4>([&](auto U) { body(kt + decltype(U)::value, U, std::true_type{}); });
 #pragma unroll
-            for (int i = 0; i < 8; ++i) qf[i] = frag(q_at[i]);
+                for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
+                    for (int h = 0; h < 2; ++h) ids[i][h] = ids_next[i][h];
+            }
+            static_for<4>([&](auto U) {
+                if (kt + decltype(U)::value < KT) body(kt + decltype(U)::value, U, std::false_type{});
+            });
+            // (the last hand-over read fragments that nobody multiplies)
+            lds_wait<0>();
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qf[i], pf[j], acc[i][j], 0, 0, 0);
-            __syncthreads();
+            for (int j = 0; j < 4; ++j) {
+                landed(pf[0][j]);
+                landed(pf[1][j]);
+                landed(qf[j]);
+            }
+        } else {
+            __builtin_amdgcn_s_barrier();  // (every wavefront has read next_tile)
+        }
+        if (wave == 0) {
+            if (queues) {
+                next_tile = dry < 8 ? (int)claimed(__builtin_amdgcn_readfirstlane(ahead)) : -1;
+            } else {
+                mine += gridDim.x;
+                next_tile = mine < total ? (int)mine : -1;
+            }
         }
         // A lane holds columns 4 g16 .. + 3 of q's group i and column l16 of p's group j.  Two neighbouring groups are
         // regrouped (lane_swap_pairs): quarter g then has columns 8 g .. 8 g + 7 of the 32, 16 bytes of an output row.
         const bool aligned = w.n_out % 8 == 0;
+        const int lane_e = opaque(lane);
 #pragma unroll
         for (int i = 0; i < 8; i += 2) {
             const int col = n0 + wn * 128 + i * 16;  // of q, a multiple of 32
             const int sel = PAIR ? (col >> 5) & 1 : 0;
-            const int c = (PAIR ? (col >> 6) * 32 : col) + g16 * 8;
+            const int c = (PAIR ? (col >> 6) * 32 : col) + (lane_e >> 4) * 8;
             bf16_t* out = w.out[sel] + (size_t)e * w.m_out * w.n_out;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -142,7 +274,7 @@ __global__ __launch_bounds__(512, 2) void weight_grad_kernel(WeightGrad w) {
                 unsigned qy = pack_bf16x2(acc[i + 1][j][2], acc[i + 1][j][3]);
                 lane_swap_pairs(px, qx);
                 lane_swap_pairs(py, qy);
-                const int m = m0 + wm * 64 + j * 16 + l16;
+                const int m = m0 + wm * 64 + j * 16 + (lane_e & 15);
                 if (m >= w.m_out) continue;
                 bf16_t* to = out + (size_t)m * w.n_out + c;
                 const u32x4 v = {px, py, qx, qy};
@@ -156,4 +288,16 @@ __global__ __launch_bounds__(512, 2) void weight_grad_kernel(WeightGrad w) {
             }
         }
     }
+}
+
+// The gradients of the first product's matrices and of the second's in one launch: a workgroup that finds no tile of the first left
+// goes on to the second.
+template <bool PAIR>
+__global__ __launch_bounds__(512, 2) void weight_grads_kernel(WeightGrad w13, WeightGrad w2, const int32_t* __restrict__ bases,
+                                                              int32_t* __restrict__ queues, int E) {
+    extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+    if (bases) order_experts((int*)(smem + kGradOrderAt), (int*)smem, bases, E);
+    weight_grad<PAIR, true>(w13, bases, queues, E, smem);
+    __builtin_amdgcn_s_barrier();  // (the number of the next tile is written again)
+    weight_grad<false, false>(w2, bases, queues ? queues + 8 : nullptr, E, smem);
 }
