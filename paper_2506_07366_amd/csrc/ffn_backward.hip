@@ -310,9 +310,22 @@ static bool backward_in_range(int T, int k, int d, int ffn, int E, int nseg, int
 // workgroups of a launch that goes round its tiles
 static unsigned tile_grid(int64_t tiles) { return (unsigned)(tiles < 1 ? 1 : tiles < (1 << 20) ? tiles : 1 << 20); }
 
+// Rows per expert, on average, up to which the gradients of the weights are made by small tiles.  Whole calls, us, large tiles -> small,
+// popularity 10 / 0.1: 128 experts of 4096 x 1536, 0.1 rows per expert 1368 -> 1066 / 1337 -> 1064, 8 2686 -> 2141 / 1632 -> 1328, 32
+// 2925 -> 2668 / 1927 -> 1712, 128 3462 -> 3713 / 2544 -> 2993; 8 of 4096 x 14336, 8 1745 -> 1430 / 1255 -> 1007, 32 1838 -> 1592 /
+// 1258 -> 1120, 128 2122 -> 2046 / 1595 -> 1591; 64 of 2048 x 1408, 12 575 -> 505 / 561 -> 491, 48 747 -> 726 / 763 -> 732, 96 879 ->
+// 887 / 862 -> 903; 64 of 768 x 3072 (ReLU), 8 378 -> 310 / 257 -> 239, 32 439 -> 418 / 316 -> 351, 64 474 -> 487 / 368 -> 452.
+// The results are the same bits: either sums an expert's rows 32 at a time in their order.
+constexpr int kFewRows = 32;
+
 template <bool PAIR>
-static int launch_weight_grads(const WeightGrad& w13, const WeightGrad& w2, const int32_t* bases, int32_t* queues, int E,
+static int launch_weight_grads(const WeightGrad& w13, const WeightGrad& w2, const int32_t* bases, int32_t* queues, int64_t A, int E,
                                hipStream_t st) {
+    if (A <= (int64_t)kFewRows * E) {
+        const int64_t tiles13 = few_rows_tiles(w13, E), tiles = tiles13 + few_rows_tiles(w2, E);
+        hipLaunchKernelGGL(few_rows_grads_kernel<PAIR>, dim3(tile_grid(tiles)), dim3(256), 0, st, w13, w2, bases, tiles13, tiles);
+        return check_launch();
+    }
     const auto kern = weight_grads_kernel<PAIR>;
     static std::atomic<unsigned long long> raised{0};
     if (const int rc = raise_lds((const void*)kern, grad_lds(MOE_MAX_EXPERTS), raised); rc != MOE_OK) return rc;
@@ -379,9 +392,9 @@ static int backward_bf16(const moe_ffn_backward_args& a, const bf16_t* x, const 
         const WeightGrad w13{x, dab, ws.tokens, d, n1 * fp, {(bf16_t*)a.dW1, (bf16_t*)a.dW3}, d, n1 * fp, d, a.ffn};
         const WeightGrad w2{hidden, (const bf16_t*)a.dy_perm, ws.rows, fp, d, {(bf16_t*)a.dW2, nullptr}, fp, d, a.ffn, d};
         const int32_t* bases = a.T > 0 ? ws.bases : nullptr;
-        int32_t* queues = a.T > 0 ? ws.queues + 24 : nullptr;
-        rc = a.relu ? launch_weight_grads<false>(w13, w2, bases, queues, a.E, st)
-                    : launch_weight_grads<true>(w13, w2, bases, queues, a.E, st);
+        const int64_t A = (int64_t)a.T * a.k;
+        rc = a.relu ? launch_weight_grads<false>(w13, w2, bases, ws.queues + 24, A, a.E, st)
+                    : launch_weight_grads<true>(w13, w2, bases, ws.queues + 24, A, a.E, st);
     }
     if (rc == MOE_OK && a.T > 0 && a.dx_perm) {
         const RowMap to_row{nullptr, nullptr, 1, ws.rows, nullptr, nullptr};

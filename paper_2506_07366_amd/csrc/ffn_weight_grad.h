@@ -66,8 +66,37 @@ __device__ __forceinline__ void order_experts(int* order, int* count, const int3
     __syncthreads();
 }
 
+// Results of 16 * J columns of p from m0 on by two neighbouring groups of q's columns, from n0 (a multiple of 32) on.  A lane holds
+// columns 4 g .. + 3 of a group of q (g the quarter of the wavefront) and column l16 of p's group j.  The two groups are
+// regrouped (lane_swap_pairs): quarter g then has columns 8 g .. 8 g + 7 of the 32, 16 bytes of an output row.
+template <bool PAIR, int J>
+__device__ __forceinline__ void store_grads(const WeightGrad& w, int e, int m0, int n0, const f32x4 (&v0)[J], const f32x4 (&v1)[J],
+                                            int lane) {
+    const bool aligned = w.n_out % 8 == 0;
+    const int c = (PAIR ? (n0 >> 6) * 32 : n0) + (lane >> 4) * 8;
+    bf16_t* out = w.out[PAIR ? (n0 >> 5) & 1 : 0] + (size_t)e * w.m_out * w.n_out;
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+        unsigned px = pack_bf16x2(v0[j][0], v0[j][1]), py = pack_bf16x2(v0[j][2], v0[j][3]);
+        unsigned qx = pack_bf16x2(v1[j][0], v1[j][1]), qy = pack_bf16x2(v1[j][2], v1[j][3]);
+        lane_swap_pairs(px, qx);
+        lane_swap_pairs(py, qy);
+        const int m = m0 + j * 16 + (lane & 15);
+        if (m >= w.m_out) continue;
+        bf16_t* to = out + (size_t)m * w.n_out + c;
+        const u32x4 v = {px, py, qx, qy};
+        if (aligned) {
+            if (c < w.n_out) *(u32x4*)to = v;
+        } else {
+#pragma unroll
+            for (int q = 0; q < 8; ++q)
+                if (c + q < w.n_out) to[q] = (bf16_t)(v[q >> 1] >> (16 * (q & 1)));
+        }
+    }
+}
+
 // PAIR: columns of q are packed pairs in blocks of 32 (of one matrix, then of the other).  P_LISTED: the rows of p go through the
-// list, those of q are in place; else the reverse.  bases, queues null: there are no rows, and the tiles are dealt out evenly.
+// list, those of q are in place; else the reverse.
 template <bool PAIR, bool P_LISTED>
 __device__ __forceinline__ void weight_grad(const WeightGrad& w, const int32_t* bases, int32_t* queues, int E,
                                             unsigned char* smem) {
@@ -87,7 +116,6 @@ __device__ __forceinline__ void weight_grad(const WeightGrad& w, const int32_t* 
     // the next XCD's.  The first claim of a workgroup is made in advance.
     constexpr int run = kGemmGrid / 8;
     int counter = blockIdx.x & 7, dry = 0;
-    int64_t mine = blockIdx.x;  // without counters
     auto claimed = [&](int i) {  // tile of claim i of the counter, claiming on where it has run out; -1: no tile is left
         for (;;) {
             const int64_t t = ((int64_t)counter + 8 * (int64_t)(i / run)) * run + i % run;
@@ -100,7 +128,7 @@ __device__ __forceinline__ void weight_grad(const WeightGrad& w, const int32_t* 
         }
     };
     // (a tile number fits: the gradients of more than 2^31 tiles would be 2^48 bytes)
-    if (wave == 0) next_tile = queues ? (int)claimed((int)(blockIdx.x >> 3)) : mine < total ? (int)mine : -1;
+    if (wave == 0) next_tile = (int)claimed((int)(blockIdx.x >> 3));
 
     for (;;) {
         lds_wait<0>();
@@ -108,14 +136,12 @@ __device__ __forceinline__ void weight_grad(const WeightGrad& w, const int32_t* 
         const int tile = lds_uniform(lds_base + kGradNextAt);
         if (tile < 0) break;
         int ahead = 0;  // the claim for the tile after this one, looked at behind the sum
-        if (queues && wave == 0 && lane == 0 && dry < 8) ahead = atomicAdd(&queues[counter], 1);
+        if (wave == 0 && lane == 0 && dry < 8) ahead = atomicAdd(&queues[counter], 1);
         const int nth = tile / per_expert, in_e = tile - nth * per_expert;
-        const int e = bases ? lds_uniform(lds_base + kGradOrderAt + (unsigned)nth * 4u) : nth;
-        // four tiles side by side along n, down all of m, and so on
-        const int group = in_e / (m_tiles * kTileGroup), in_g = in_e - group * (m_tiles * kTileGroup);
-        const int gw = n_tiles - group * kTileGroup < kTileGroup ? n_tiles - group * kTileGroup : kTileGroup;
-        const int n0 = (group * kTileGroup + in_g % gw) * kGradTile, m0 = in_g / gw * kGradTile;
-        const int first = bases ? bases[e] : 0, last = bases ? bases[e + 1] : 0;
+        const int e = lds_uniform(lds_base + kGradOrderAt + (unsigned)nth * 4u);
+        // along n first: what is written at a time is whole rows of the matrix (four tiles side by side, down all of m: 0 to 4 % slower)
+        const int n0 = in_e % n_tiles * kGradTile, m0 = in_e / n_tiles * kGradTile;
+        const int first = bases[e], last = bases[e + 1];
         const int KT = ceil_div(last - first, kGradRows);
 
         // Loads: instruction i of a wavefront brings rows 2 (wave + 8 i) and + 1 of the step, 512 bytes each.
@@ -249,44 +275,11 @@ __device__ __forceinline__ void weight_grad(const WeightGrad& w, const int32_t* 
         } else {
             __builtin_amdgcn_s_barrier();  // (every wavefront has read next_tile)
         }
-        if (wave == 0) {
-            if (queues) {
-                next_tile = dry < 8 ? (int)claimed(__builtin_amdgcn_readfirstlane(ahead)) : -1;
-            } else {
-                mine += gridDim.x;
-                next_tile = mine < total ? (int)mine : -1;
-            }
-        }
-        // A lane holds columns 4 g16 .. + 3 of q's group i and column l16 of p's group j.  Two neighbouring groups are
-        // regrouped (lane_swap_pairs): quarter g then has columns 8 g .. 8 g + 7 of the 32, 16 bytes of an output row.
-        const bool aligned = w.n_out % 8 == 0;
+        if (wave == 0) next_tile = dry < 8 ? (int)claimed(__builtin_amdgcn_readfirstlane(ahead)) : -1;
         const int lane_e = opaque(lane);
 #pragma unroll
-        for (int i = 0; i < 8; i += 2) {
-            const int col = n0 + wn * 128 + i * 16;  // of q, a multiple of 32
-            const int sel = PAIR ? (col >> 5) & 1 : 0;
-            const int c = (PAIR ? (col >> 6) * 32 : col) + (lane_e >> 4) * 8;
-            bf16_t* out = w.out[sel] + (size_t)e * w.m_out * w.n_out;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                unsigned px = pack_bf16x2(acc[i][j][0], acc[i][j][1]), py = pack_bf16x2(acc[i][j][2], acc[i][j][3]);
-                unsigned qx = pack_bf16x2(acc[i + 1][j][0], acc[i + 1][j][1]);
-                unsigned qy = pack_bf16x2(acc[i + 1][j][2], acc[i + 1][j][3]);
-                lane_swap_pairs(px, qx);
-                lane_swap_pairs(py, qy);
-                const int m = m0 + wm * 64 + j * 16 + (lane_e & 15);
-                if (m >= w.m_out) continue;
-                bf16_t* to = out + (size_t)m * w.n_out + c;
-                const u32x4 v = {px, py, qx, qy};
-                if (aligned) {
-                    if (c < w.n_out) *(u32x4*)to = v;
-                } else {
-#pragma unroll
-                    for (int q = 0; q < 8; ++q)
-                        if (c + q < w.n_out) to[q] = (bf16_t)(v[q >> 1] >> (16 * (q & 1)));
-                }
-            }
-        }
+        for (int i = 0; i < 8; i += 2)
+            store_grads<PAIR, 4>(w, e, m0 + wm * 64, n0 + wn * 128 + i * 16, acc[i], acc[i + 1], lane_e);
     }
 }
 
@@ -296,8 +289,119 @@ template <bool PAIR>
 __global__ __launch_bounds__(512, 2) void weight_grads_kernel(WeightGrad w13, WeightGrad w2, const int32_t* __restrict__ bases,
                                                               int32_t* __restrict__ queues, int E) {
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
-    if (bases) order_experts((int*)(smem + kGradOrderAt), (int*)smem, bases, E);
+    order_experts((int*)(smem + kGradOrderAt), (int*)smem, bases, E);
     weight_grad<PAIR, true>(w13, bases, queues, E, smem);
     __builtin_amdgcn_s_barrier();  // (the number of the next tile is written again)
-    weight_grad<false, false>(w2, bases, queues ? queues + 8 : nullptr, E, smem);
+    weight_grad<false, false>(w2, bases, queues + 8, E, smem);
+}
+
+// ---------------------------------------------------------------------------
+// few rows per expert
+// ---------------------------------------------------------------------------
+// What bounds the gradients then is writing them, and a tile is little more than its start, a step or two, and its stores.  So tiles
+// are small, 64 of m by 256 of n, four workgroups share a CU, none waits for another, and tiles without rows are stores
+// alone.  A wavefront has all of m by 64 of n.  Two steps of 32 rows have room in LDS.  128 tokens, top-8 of 128 experts of 4096 x
+// 1536 (4.8 GB of gradients): 1403 us with the tiles above, 1240 with half as high ones and two workgroups on a CU.
+constexpr int kFewM = 64, kFewN = 256, kFewStages = 2;
+constexpr int kFewPanelM = kGradRows * kFewM * 2, kFewPanelN = kGradRows * kFewN * 2, kFewStage = kFewPanelM + kFewPanelN;
+
+// bases null: there are no rows.
+template <bool PAIR, bool P_LISTED>
+__device__ __forceinline__ void few_rows_tile(const WeightGrad& w, const int32_t* bases, int64_t tile, unsigned char* smem) {
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int m_tiles = ceil_div(w.M, kFewM), n_tiles = ceil_div(w.N, kFewN);
+    const int e = (int)(tile / ((int64_t)m_tiles * n_tiles));
+    const int in_e = (int)(tile - (int64_t)e * ((int64_t)m_tiles * n_tiles));
+    const int n0 = in_e % n_tiles * kFewN, m0 = in_e / n_tiles * kFewM;
+    const int first = bases ? bases[e] : 0, rows = bases ? bases[e + 1] - first : 0;
+    const int KT = ceil_div(rows, kGradRows);
+    const unsigned lds_base = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)smem;
+
+    f32x4 acc[4][4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+    if (KT > 0) {
+        // Loads: a wavefront brings 8 rows of p's panel (128 bytes each) with one instruction, and with four rows 2 (wave + 4 i) and + 1
+        // of q's (512 bytes).  Pieces of 32 bytes stand at piece ^ ((row >> 1) & 3) and piece ^ (row & 7): see above.
+        constexpr unsigned kRange = 0xffffff80u, kPast = 0xfffffff0u;
+        const int row_p = 8 * wave + (lane >> 3), row_q = 2 * wave + (lane >> 5);
+        const int at_p = m0 + ((lane & 7) ^ (((row_p >> 1) & 3) << 1)) * 8, at_q = n0 + ((lane & 31) ^ ((row_q & 7) << 1)) * 8;
+        const auto p_rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)w.p, 0, (int)kRange, 0x00027000);
+        const auto q_rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)w.q, 0, (int)kRange, 0x00027000);
+        const auto p_here = __builtin_amdgcn_make_buffer_rsrc((void*)(w.p + (size_t)first * w.ldp), 0, (int)kRange, 0x00027000);
+        const auto q_here = __builtin_amdgcn_make_buffer_rsrc((void*)(w.q + (size_t)first * w.ldq), 0, (int)kRange, 0x00027000);
+        auto load = [&](int kt) {
+            unsigned char* to = smem + (kt & 1) * kFewStage;
+            const int rp = kt * kGradRows + row_p;
+            unsigned off = kPast;  // past the rows and the columns: zeros
+            if (rp < rows && at_p < w.M)
+                off = ((unsigned)(P_LISTED ? w.rows[first + rp] : rp) * (unsigned)w.ldp + (unsigned)at_p) * 2u;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(P_LISTED ? p_rsrc : p_here,
+                                                     (__attribute__((address_space(3))) void*)(to + wave * 1024), 16, off, 0, 0, 0);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int rq = kt * kGradRows + row_q + 8 * i;
+                off = kPast;
+                if (rq < rows && at_q < w.N)
+                    off = ((unsigned)(P_LISTED ? rq : w.rows[first + rq]) * (unsigned)w.ldq + (unsigned)at_q) * 2u;
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(
+                    P_LISTED ? q_here : q_rsrc,
+                    (__attribute__((address_space(3))) void*)(to + kFewPanelM + (wave + 4 * i) * 1024), 16, off, 0, 0, 0);
+            }
+        };
+        const int l16 = lane & 15, g16 = lane >> 4, rr = 4 * g16 + (l16 >> 2);
+        const unsigned at = lds_base + (l16 & 3) * 8;
+        load(0);
+        for (int kt = 0; kt < KT; ++kt) {
+            if (kt + 1 < KT) load(kt + 1);
+            __builtin_amdgcn_sched_barrier(0);
+            if (kt + 1 < KT) wait_vmcnt<5>();  // (the loads of the next step)
+            else wait_vmcnt<0>();
+            __builtin_amdgcn_s_barrier();
+            const unsigned stage = at + (unsigned)((kt & 1) * kFewStage);
+            GradFrag pf[4], qf[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const unsigned p = stage + (unsigned)(rr * (kFewM * 2) + (i ^ ((rr >> 1) & 3)) * 32);
+                const unsigned q = stage + (unsigned)(kFewPanelM + rr * (kFewN * 2) + (wave >> 1) * 256 +
+                                                      (((wave & 1) * 4 + i) ^ (rr & 7)) * 32);
+                lds_read_tr<0>(pf[i].lo, p);
+                lds_read_tr<16 * kFewM * 2>(pf[i].hi, p);
+                lds_read_tr<0>(qf[i].lo, q);
+                lds_read_tr<16 * kFewN * 2>(qf[i].hi, q);
+            }
+            lds_wait<0>();
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                landed(pf[i]);
+                landed(qf[i]);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(whole(qf[i]), whole(pf[j]), acc[i][j], 0, 0, 0);
+            __builtin_amdgcn_s_barrier();  // everybody has read the stage
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; i += 2) store_grads<PAIR, 4>(w, e, m0, n0 + wave * 64 + i * 16, acc[i], acc[i + 1], lane);
+}
+
+template <bool PAIR>
+__global__ __launch_bounds__(256, 4) void few_rows_grads_kernel(WeightGrad w13, WeightGrad w2, const int32_t* __restrict__ bases,
+                                                                int64_t tiles13, int64_t tiles) {
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[kFewStages * kFewStage];
+    for (int64_t t = blockIdx.x; t < tiles; t += gridDim.x) {
+        if (t < tiles13) few_rows_tile<PAIR, true>(w13, bases, t, smem);
+        else few_rows_tile<false, false>(w2, bases, t - tiles13, smem);
+    }
+}
+inline int64_t few_rows_tiles(const WeightGrad& w, int E) {
+    return (int64_t)E * ceil_div(w.M, kFewM) * ceil_div(w.N, kFewN);
 }

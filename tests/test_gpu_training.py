@@ -328,6 +328,29 @@ def test_ffn_backward_bf16_odd_widths(d, ffn):
     check_ffn(c, run_ffn(c))
 
 
+@pytest.mark.parametrize("d,ffn", [(64, 1), (64, 7), (128, 65), (192, 130), (64, 520), (576, 66)])
+@pytest.mark.parametrize("rows", [[97, 0, 0, 128, 5], [65, 66, 1, 0, 161]])
+def test_ffn_backward_bf16_odd_widths_of_many_rows(d, ffn, rows):
+    """More than 32 rows per expert on average: the weights' gradients by large tiles.  Experts without rows and with few among them;
+    the last of an expert's steps of 32 rows is first, second, third and fourth of four, whole and of one row."""
+    for relu in (False, True):
+        c = ffn_case(rows, [1, 4, 2, 0, 3], 5, 1, d, ffn, "bf16", relu, seed=ffn + rows[0])
+        check_ffn(c, run_ffn(c))
+
+
+def test_ffn_backward_is_the_same_on_either_side_of_the_tile_rule():
+    """The gradients of an expert do not depend on how many other experts there are: 33 rows per expert on average, and fewer."""
+    c = ffn_case([40, 26], [0, 1], 2, 1, 128, 200, "bf16", False, seed=21)
+    got = run_ffn(c)
+    wide = dict(c, E=9)
+    for name in ("W1", "W3", "W2"):
+        wide[name] = torch.cat([c[name], torch.zeros((7, *c[name].shape[1:]), dtype=torch.bfloat16, device="cuda")])
+    many = run_ffn(wide)
+    assert torch.equal(many[0], got[0])
+    for a, b in zip(many[1:], got[1:]):
+        assert torch.equal(a[:2], b) and torch.all(a[2:] == 0)
+
+
 @pytest.mark.parametrize("d,ffn", [(4, 4), (12, 20), (132, 68)])
 def test_ffn_backward_f32_narrow(d, ffn):
     for relu in (False, True):
