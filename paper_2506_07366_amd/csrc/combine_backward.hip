@@ -70,8 +70,14 @@ __global__ __launch_bounds__(1024) void combine_backward_kernel(CombineBackward 
         float w[KMAX], dot[KMAX];
 #pragma unroll
         for (int j = 0; j < KMAX; ++j) {
-            rows[j] = j < a.k ? a.row_of_assign[(size_t)t * a.k + j] : 0;
-            w[j] = j < a.k ? a.topk_w[(size_t)t * a.k + j] : 0.f;
+            if constexpr (KMAX <= 8) {  // all asked for at once: one token 9.2 -> 8.5 us (with 16 of them they leave the registers)
+                const size_t at = (size_t)t * a.k + (j < a.k ? j : a.k - 1);
+                rows[j] = a.row_of_assign[at];
+                w[j] = a.topk_w[at];
+            } else {
+                rows[j] = j < a.k ? a.row_of_assign[(size_t)t * a.k + j] : 0;
+                w[j] = j < a.k ? a.topk_w[(size_t)t * a.k + j] : 0.f;
+            }
             dot[j] = 0.f;
         }
         for (int p = (int)threadIdx.x; p < a.pieces; p += blockDim.x) {
