@@ -12,6 +12,12 @@
 // LDS, three are under way; the rows of the listed operand are looked up four steps ahead of its loads.  A step is eight
 // fragments of Q against four of P; the hand-over to the next step stands two fragments before the end, so that its first
 // reads land under what is left to multiply.
+//
+// 8192 rows of 8 experts of 4096 x 14336: 2.98 ms, 0.97 PFLOP/s; 98304 of 64 of 2048 x 1408: 1.71 ms, 0.99.  A step takes 0.96 us, of
+// which the transposing reads (96 KiB, at half the rate of 16-byte ones) need 0.6 and the matrix pipe 0.8 at the rate of a large
+// product; a tile's stores, made by all workgroups at about the same time, come on top (0.4 ms of the 2.98).  Two
+// workgroups on a CU with half as high tiles, and the next tile's first steps asked for ahead of the stores, were 3 % slower there
+// and 12 to 17 % on the second shape, four wavefronts of 128 x 128 a third.
 #pragma once
 
 struct WeightGrad {
