@@ -307,7 +307,18 @@ def moe_packed_weights_bytes(E: int, d: int, ffn: int, dtype: int) -> int:
     return int(load_library().moe_packed_weights_bytes(E, d, ffn, dtype))
 
 
-def moe_pack_weights(W1: torch.Tensor, W3: torch.Tensor, W2: torch.Tensor) -> torch.Tensor:
+def _room(out: Optional[torch.Tensor], n: int, device) -> torch.Tensor:
+    """``out``, or a new buffer, for n bytes of packed weights."""
+    if out is None:
+        return torch.empty(n, dtype=torch.uint8, device=device)
+    if _need(out, torch.uint8, "out").numel() != n:
+        raise MoeGpsError(f"out must hold the packed weights' {n} bytes, got {out.numel()}")
+    return out
+
+
+def moe_pack_weights(W1: torch.Tensor, W3: torch.Tensor, W2: torch.Tensor,
+                     out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Weights laid out for the FFN.  ``out``: optional buffer of moe_packed_weights_bytes to write into."""
     lib = load_library()
     dt = dtype_code(W1)
     for name, t in (("W1", W1), ("W3", W3), ("W2", W2)):
@@ -315,7 +326,7 @@ def moe_pack_weights(W1: torch.Tensor, W3: torch.Tensor, W2: torch.Tensor) -> to
     E, d, ffn = W1.shape
     if tuple(W3.shape) != (E, d, ffn) or tuple(W2.shape) != (E, ffn, d):
         raise MoeGpsError("weight shapes must be W1,W3 [E,d,ffn] and W2 [E,ffn,d]")
-    packed = torch.empty(moe_packed_weights_bytes(E, d, ffn, dt), dtype=torch.uint8, device=W1.device)
+    packed = _room(out, moe_packed_weights_bytes(E, d, ffn, dt), W1.device)
     _check(lib.moe_pack_weights(_ptr(W1), _ptr(W3), _ptr(W2), dt, E, d, ffn, _ptr(packed), _stream()),
            "moe_pack_weights")
     return packed
@@ -325,15 +336,15 @@ def moe_grouped_ffn_workspace_bytes(A: int, d: int, ffn: int, nseg: int, dtype: 
     return int(load_library().moe_grouped_ffn_workspace_bytes(A, d, ffn, nseg, dtype))
 
 
-def moe_pack_weights_relu(W1: torch.Tensor, W2: torch.Tensor) -> torch.Tensor:
-    """Packed weights of the ReLU form of the FFN (W1 [E, d, ffn], W2 [E, ffn, d])."""
+def moe_pack_weights_relu(W1: torch.Tensor, W2: torch.Tensor, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Packed weights of the ReLU form of the FFN (W1 [E, d, ffn], W2 [E, ffn, d]); ``out``: optional buffer for them."""
     lib = load_library()
     dt = dtype_code(W1)
     _need(W2, W1.dtype, "W2")
     E, d, ffn = W1.shape
     if tuple(W2.shape) != (E, ffn, d):
         raise MoeGpsError("weight shapes must be W1 [E,d,ffn] and W2 [E,ffn,d]")
-    packed = torch.empty(int(lib.moe_packed_weights_relu_bytes(E, d, ffn, dt)), dtype=torch.uint8, device=W1.device)
+    packed = _room(out, int(lib.moe_packed_weights_relu_bytes(E, d, ffn, dt)), W1.device)
     _check(lib.moe_pack_weights_relu(_ptr(W1), _ptr(W2), dt, E, d, ffn, _ptr(packed), _stream()),
            "moe_pack_weights_relu")
     return packed
@@ -516,8 +527,10 @@ def moe_packed_weights_backward_bytes(E: int, d: int, ffn: int, dtype: int, relu
     return int(load_library().moe_packed_weights_backward_bytes(E, d, ffn, dtype, relu))
 
 
-def moe_pack_weights_backward(W1: torch.Tensor, W3: Optional[torch.Tensor], W2: torch.Tensor) -> torch.Tensor:
-    """Weights laid out for the backward pass (W3 None: the ReLU form); empty for fp32, which needs none."""
+def moe_pack_weights_backward(W1: torch.Tensor, W3: Optional[torch.Tensor], W2: torch.Tensor,
+                              out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Weights laid out for the backward pass (W3 None: the ReLU form); empty for fp32, which needs none.  ``out``: optional
+    buffer of moe_packed_weights_backward_bytes to write into."""
     lib = load_library()
     dt = dtype_code(W1)
     for name, t in (("W1", W1), ("W3", W3), ("W2", W2)):
@@ -526,8 +539,7 @@ def moe_pack_weights_backward(W1: torch.Tensor, W3: Optional[torch.Tensor], W2: 
     E, d, ffn = W1.shape
     if (W3 is not None and tuple(W3.shape) != (E, d, ffn)) or tuple(W2.shape) != (E, ffn, d):
         raise MoeGpsError("weight shapes must be W1,W3 [E,d,ffn] and W2 [E,ffn,d]")
-    packed = torch.empty(moe_packed_weights_backward_bytes(E, d, ffn, dt, W3 is None), dtype=torch.uint8,
-                         device=W1.device)
+    packed = _room(out, moe_packed_weights_backward_bytes(E, d, ffn, dt, W3 is None), W1.device)
     _check(lib.moe_pack_weights_backward(_ptr(W1), _ptr(W3), _ptr(W2), dt, E, d, ffn, _ptr(packed), _stream()),
            "moe_pack_weights_backward")
     return packed

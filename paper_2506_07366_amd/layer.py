@@ -65,15 +65,22 @@ class MoELayer:
         self.ws_ffn = torch.empty(max(256, B.moe_grouped_ffn_workspace_bytes(c.A, c.d, c.ffn, c.nseg, dcode)),
                                   dtype=torch.uint8, device=self.dev)
         self.packed: Optional[torch.Tensor] = None
+        self.in_training = False   # a MoETraining stands beside this layer (training.py)
+        self._packed_place: Optional[torch.Tensor] = None
 
     def set_weights(self, W1: torch.Tensor, W3: Optional[torch.Tensor], W2: torch.Tensor) -> None:
-        """One-off repack of the (static) expert weights; the ReLU form has no W3."""
+        """One-off repack of the (static) expert weights, into a new buffer; the ReLU form has no W3.  In training, where
+        they change, they are laid out in the same buffer every time: a recorded graph reads those set last."""
+        if self.cfg.act == "relu" and self.fused_gather:
+            raise B.MoeGpsError("the fused row gather is built for the SwiGLU form only")
+        # (a buffer that came from elsewhere, another layer's, is not written over)
+        place = self.packed if self.packed is not None and self.packed is self._packed_place else None
         if self.cfg.act == "relu":
-            if self.fused_gather:
-                raise B.MoeGpsError("the fused row gather is built for the SwiGLU form only")
-            self.packed = B.moe_pack_weights_relu(W1, W2)
+            self.packed = B.moe_pack_weights_relu(W1, W2, out=place)
         else:
-            self.packed = B.moe_pack_weights(W1, W3, W2)
+            self.packed = B.moe_pack_weights(W1, W3, W2, out=place)
+        if self.in_training:
+            self._packed_place = self.packed
 
     # individual steps (each is exactly one C-ABI call) ---------------------
     def route(self, logits):

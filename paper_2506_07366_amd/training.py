@@ -7,8 +7,8 @@ and the experts' results, in 8 bits (``moe_checkpoint_store``) or as they are; `
     moe_grouped_ffn_backward  dx_perm, gradients of the expert weights (hidden activations worked out again)
     moe_combine               dx
 
-with no host synchronisation; buffers are allocated once, so ``save`` and ``backward`` can be recorded into a HIP graph after
-one eager run.  The paper trains nothing; the plan only says where a row is computed and has no gradient.
+with no host synchronisation; buffers are allocated once, those of the weights with the first ``set_weights``, so ``save`` and
+``backward`` can be recorded into a HIP graph after one eager run, which then reads the weights set last.  The paper trains nothing; the plan only says where a row is computed and has no gradient.
 
 ``python -m paper_2506_07366_amd.training`` fits a small layer to another one's outputs.
 """
@@ -32,6 +32,7 @@ class MoETraining:
             raise B.MoeGpsError("a layer with fused_weights keeps y_perm with the gate weights applied: its gradient needs "
                                 "the rows without them")
         self.layer = layer
+        layer.in_training = True
         self.saved = saved
         c = layer.cfg
         dt = torch_dtype(c)
@@ -57,9 +58,10 @@ class MoETraining:
         self.packed_backward: Optional[torch.Tensor] = None
 
     def set_weights(self, W1: torch.Tensor, W3: Optional[torch.Tensor], W2: torch.Tensor) -> None:
-        """Lays the weights out for both passes, whenever they have changed."""
+        """Lays the weights out for both passes, whenever they have changed; in the same buffers every time, in stream order."""
         self.layer.set_weights(W1, W3, W2)
-        self.packed_backward = B.moe_pack_weights_backward(W1, None if self.layer.cfg.act == "relu" else W3, W2)
+        self.packed_backward = B.moe_pack_weights_backward(W1, None if self.layer.cfg.act == "relu" else W3, W2,
+                                                           out=self.packed_backward)
 
     def save(self, x: torch.Tensor) -> None:
         """Keeps what the backward pass of the layer's last step reads; x: the step's input rows."""

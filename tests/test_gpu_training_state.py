@@ -1,0 +1,46 @@
+"""What a training step keeps from one call to the next: the routing of the saved batch, both layouts of the weights, the
+places that a recorded graph reads."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2506_07366_amd.layer import MoELayer
+from paper_2506_07366_amd.training import MoETraining
+from test_gpu_training_layer import make, step
+
+pytestmark = pytest.mark.gpu
+
+
+def clones(grads):
+    return {n: None if v is None else v.clone() for n, v in grads.items()}
+
+
+def same(got, want):
+    for n, v in want.items():
+        assert (got[n] is None) == (v is None) and (v is None or torch.equal(got[n], v)), n
+
+
+@pytest.mark.parametrize("dtype,act", [("f32", "swiglu"), ("bf16", "swiglu"), ("bf16", "relu")])
+def test_graph_of_a_step_and_weights_that_change(dtype, act):
+    """A recorded training step reads the weights set last: they are laid out in the same place every time."""
+    c = make(100, 2, 8, 4, 3, 128, 72, dtype, act=act)
+    train, layer = c["train"], c["layer"]
+    step(c)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step(c)
+    at = (layer.packed.data_ptr(), train.packed_backward.data_ptr())
+    size = layer.packed.numel() + train.packed_backward.numel()
+    for i in range(3):
+        W = [None if c[n] is None else (-0.5 * c[n]).roll(i + 1, dims=0).contiguous() for n in ("W1", "W3", "W2")]
+        train.set_weights(*W)
+        # (first: nothing is replayed that would read freed memory)
+        assert (layer.packed.data_ptr(), train.packed_backward.data_ptr()) == at
+        torch.full((size,), 0xff, dtype=torch.uint8, device="cuda")  # what takes the place of anything freed
+        graph.replay()
+        torch.cuda.synchronize()
+        replayed = clones(got)
+        other = MoETraining(MoELayer(c["cfg"]))
+        other.set_weights(*W)
+        same(replayed, step(dict(c, layer=other.layer, train=other)))
