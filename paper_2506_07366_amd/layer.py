@@ -66,21 +66,25 @@ class MoELayer:
                                   dtype=torch.uint8, device=self.dev)
         self.packed: Optional[torch.Tensor] = None
         self.in_training = False   # a MoETraining stands beside this layer (training.py)
-        self._packed_place: Optional[torch.Tensor] = None
+        self.packed_backward: Optional[torch.Tensor] = None  # in training: the same weights as the backward pass wants them
+        self._packed_places: tuple = (None, None)  # the buffers that set_weights has made in training
 
     def set_weights(self, W1: torch.Tensor, W3: Optional[torch.Tensor], W2: torch.Tensor) -> None:
         """One-off repack of the (static) expert weights, into a new buffer; the ReLU form has no W3.  In training, where
-        they change, they are laid out in the same buffer every time: a recorded graph reads those set last."""
+        they change, they are laid out for both passes and in the same buffers every time: a recorded graph reads those set last."""
         if self.cfg.act == "relu" and self.fused_gather:
             raise B.MoeGpsError("the fused row gather is built for the SwiGLU form only")
         # (a buffer that came from elsewhere, another layer's, is not written over)
-        place = self.packed if self.packed is not None and self.packed is self._packed_place else None
+        place, place_backward = (p if p is now else None for p, now in
+                                 zip(self._packed_places, (self.packed, self.packed_backward)))
         if self.cfg.act == "relu":
             self.packed = B.moe_pack_weights_relu(W1, W2, out=place)
         else:
             self.packed = B.moe_pack_weights(W1, W3, W2, out=place)
         if self.in_training:
-            self._packed_place = self.packed
+            self.packed_backward = B.moe_pack_weights_backward(W1, None if self.cfg.act == "relu" else W3, W2,
+                                                               out=place_backward)
+            self._packed_places = self.packed, self.packed_backward
 
     # individual steps (each is exactly one C-ABI call) ---------------------
     def route(self, logits):

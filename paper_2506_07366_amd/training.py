@@ -55,13 +55,19 @@ class MoETraining:
         self.workspace = torch.empty(
             B.moe_grouped_ffn_backward_workspace_bytes(c.T, c.k, c.d, c.ffn, c.E, c.nseg, dcode, c.act == "relu"),
             dtype=torch.uint8, device=layer.dev)
-        self.packed_backward: Optional[torch.Tensor] = None
+
+    @property
+    def packed_backward(self) -> Optional[torch.Tensor]:
+        """The layer's: whoever sets its weights, both layouts are of the same ones."""
+        return self.layer.packed_backward
+
+    @packed_backward.setter
+    def packed_backward(self, packed: Optional[torch.Tensor]) -> None:
+        self.layer.packed_backward = packed
 
     def set_weights(self, W1: torch.Tensor, W3: Optional[torch.Tensor], W2: torch.Tensor) -> None:
         """Lays the weights out for both passes, whenever they have changed; in the same buffers every time, in stream order."""
         self.layer.set_weights(W1, W3, W2)
-        self.packed_backward = B.moe_pack_weights_backward(W1, None if self.layer.cfg.act == "relu" else W3, W2,
-                                                           out=self.packed_backward)
 
     def save(self, x: torch.Tensor) -> None:
         """Keeps what the backward pass of the layer's last step reads; x: the step's input rows."""

@@ -21,6 +21,19 @@ def same(got, want):
 
 
 @pytest.mark.parametrize("dtype,act", [("f32", "swiglu"), ("bf16", "swiglu"), ("bf16", "relu")])
+def test_weights_set_on_the_layer(dtype, act):
+    """Weights that are set on the layer, not on the object beside it, are those of its gradients too."""
+    c = make(150, 2, 8, 4, 3, 128, 72, dtype, act=act, mode=0)
+    step(c)
+    W = [None if c[n] is None else c[n].flip(0).contiguous() for n in ("W1", "W3", "W2")]
+    c["layer"].set_weights(*W)
+    got = clones(step(c))
+    other = MoETraining(MoELayer(c["cfg"]))
+    other.set_weights(*W)
+    same(got, step(dict(c, layer=other.layer, train=other)))
+
+
+@pytest.mark.parametrize("dtype,act", [("f32", "swiglu"), ("bf16", "swiglu"), ("bf16", "relu")])
 def test_graph_of_a_step_and_weights_that_change(dtype, act):
     """A recorded training step reads the weights set last: they are laid out in the same place every time."""
     c = make(100, 2, 8, 4, 3, 128, 72, dtype, act=act)
@@ -44,3 +57,16 @@ def test_graph_of_a_step_and_weights_that_change(dtype, act):
         other = MoETraining(MoELayer(c["cfg"]))
         other.set_weights(*W)
         same(replayed, step(dict(c, layer=other.layer, train=other)))
+
+
+def test_layouts_that_came_from_elsewhere_are_not_written_over():
+    """A layer that reads another one's weights gets buffers of its own when its weights are set."""
+    c = make(40, 2, 8, 4, 3, 128, 72, "bf16")
+    want = clones(step(c))
+    other = MoETraining(MoELayer(c["cfg"]))
+    other.layer.packed, other.packed_backward = c["layer"].packed, c["train"].packed_backward
+    shared = dict(c, layer=other.layer, train=other)
+    same(step(shared), want)
+    other.set_weights(*[2 * c[n] for n in ("W1", "W3", "W2")])
+    step(shared)
+    same(step(c), want)
