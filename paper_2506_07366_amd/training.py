@@ -24,8 +24,9 @@ from .layer import MoELayer, torch_dtype
 
 class MoETraining:
     def __init__(self, layer: MoELayer, saved: str = "8bit"):
-        """saved: "8bit" keeps x and y_perm as checkpoints (1.03 bytes a value, apart from the layer's buffers: several layers or
-        micro-batches can be under way); "plain" reads them where they are: x and the layer are left alone until backward."""
+        """saved: "8bit" keeps x and y_perm as checkpoints (1.03 bytes a value) and a copy of the step's routing, apart from the
+        layer's buffers: several layers, or several objects with a micro-batch of one layer each, can be under way; "plain" reads
+        all of it where it is: x and the layer are left alone until backward."""
         if saved not in ("8bit", "plain"):
             raise B.MoeGpsError(f"saved must be '8bit' or 'plain', got {saved!r}")
         if layer.fused_weights:
@@ -42,7 +43,8 @@ class MoETraining:
         keep = lambda rows: (torch.empty((rows, c.d), dtype=torch.float8_e4m3fn, device=layer.dev),
                              torch.empty((rows, groups), dtype=torch.uint8, device=layer.dev))
         self._kept = (keep(c.T), keep(c.A)) if saved == "8bit" else None
-        self._x = self._y = None
+        self._kept_routing = tuple(torch.empty_like(t) for t in self._live_routing()) if saved == "8bit" else None
+        self._x = self._y = self._routing = None
         self.dy_perm = torch.empty((c.A, c.d), **like)
         self.dx_perm = torch.empty((c.A, c.d), **like)
         self.dx = torch.empty((c.T, c.d), **like)
@@ -69,30 +71,39 @@ class MoETraining:
         """Lays the weights out for both passes, whenever they have changed; in the same buffers every time, in stream order."""
         self.layer.set_weights(W1, W3, W2)
 
+    def _live_routing(self) -> tuple:
+        """What backward reads of the layer's last step besides its rows: all of it 32-bit values."""
+        layer, p = self.layer, self.layer.perm
+        return (layer.topk_w, layer.topk_idx, p["row_of_assign"], p["assign_of_row"], p["seg_offsets"], layer.slot_expert)
+
     def save(self, x: torch.Tensor) -> None:
         """Keeps what the backward pass of the layer's last step reads; x: the step's input rows."""
         if self._kept is None:
-            self._x, self._y = x, self.layer.y_perm
+            self._x, self._y, self._routing = x, self.layer.y_perm, self._live_routing()
             return
         kept_x, kept_y = self._kept
         self._x = B.moe_checkpoint_store(x, out=kept_x)
         self._y = B.moe_checkpoint_store(self.layer.y_perm, out=kept_y)
+        # (one launch for all of them, and as tensors of one type)
+        torch._foreach_copy_([t.view(torch.int32) for t in self._kept_routing],
+                             [t.view(torch.int32) for t in self._live_routing()])
+        self._routing = self._kept_routing
 
     def backward(self, dout: torch.Tensor) -> dict:
         """Gradients of the saved step from that of its output: dx, dtopk_w, dlogits and those of the expert weights, in this
-        object's buffers.  Routing, permutation and plan are read from the layer: its next step comes after this."""
+        object's buffers.  The weights are those that the layer has now: they are set for the next step after this."""
         if self.packed_backward is None:
             raise B.MoeGpsError("set_weights() first")
         if self._x is None:
             raise B.MoeGpsError("save() first")
         layer, c = self.layer, self.layer.cfg
-        p = layer.perm
-        B.moe_combine_backward(dout, self._y, p["row_of_assign"], layer.topk_w, topk_idx=layer.topk_idx, E=c.E,
+        topk_w, topk_idx, row_of_assign, assign_of_row, seg_offsets, slot_expert = self._routing
+        B.moe_combine_backward(dout, self._y, row_of_assign, topk_w, topk_idx=topk_idx, E=c.E,
                                out=(self.dy_perm, self.dtopk_w, self.dlogits))
-        B.moe_grouped_ffn_backward(self._x, p["assign_of_row"], c.k, self.dy_perm, p["seg_offsets"], layer.slot_expert,
-                                   layer.packed, self.packed_backward, c.E, c.ffn, relu=c.act == "relu",
-                                   workspace=self.workspace, out=(self.dx_perm, self.dW1, self.dW3, self.dW2))
-        B.moe_combine(self.dx_perm, p["row_of_assign"], None, c.T, c.k, out=self.dx)
+        B.moe_grouped_ffn_backward(self._x, assign_of_row, c.k, self.dy_perm, seg_offsets, slot_expert, layer.packed,
+                                   self.packed_backward, c.E, c.ffn, relu=c.act == "relu", workspace=self.workspace,
+                                   out=(self.dx_perm, self.dW1, self.dW3, self.dW2))
+        B.moe_combine(self.dx_perm, row_of_assign, None, c.T, c.k, out=self.dx)
         return dict(dx=self.dx, dtopk_w=self.dtopk_w, dlogits=self.dlogits, dW1=self.dW1, dW3=self.dW3, dW2=self.dW2)
 
 
