@@ -338,24 +338,29 @@ __device__ __forceinline__ void few_rows_tile(const WeightGrad& w, const int32_t
         const int at_p = m0 + ((lane & 7) ^ (((row_p >> 1) & 3) << 1)) * 8, at_q = n0 + ((lane & 31) ^ ((row_q & 7) << 1)) * 8;
         const auto p_rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)w.p, 0, (int)kRange, 0x00027000);
         const auto q_rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)w.q, 0, (int)kRange, 0x00027000);
-        const auto p_here = __builtin_amdgcn_make_buffer_rsrc((void*)(w.p + (size_t)first * w.ldp), 0, (int)kRange, 0x00027000);
-        const auto q_here = __builtin_amdgcn_make_buffer_rsrc((void*)(w.q + (size_t)first * w.ldq), 0, (int)kRange, 0x00027000);
+        // Rows that go through the list are addressed from the start of their operand (the host checks that 32 bits reach); those in
+        // place from the step's first, as all of a batch's rows may be this expert's: 32768 of 65792 values are 2^32 bytes.
         auto load = [&](int kt) {
             unsigned char* to = smem + (kt & 1) * kFewStage;
-            const int rp = kt * kGradRows + row_p;
+            const int left = rows - kt * kGradRows;  // rows from the step's first on
+            const int p0 = first + kt * kGradRows;
+            const int32_t* list = w.rows + p0;
+            const auto here = __builtin_amdgcn_make_buffer_rsrc((void*)(P_LISTED ? w.q + (size_t)p0 * w.ldq : w.p + (size_t)p0 * w.ldp),
+                                                                0, (int)kRange, 0x00027000);
             unsigned off = kPast;  // past the rows and the columns: zeros
-            if (rp < rows && at_p < w.M)
-                off = ((unsigned)(P_LISTED ? w.rows[first + rp] : rp) * (unsigned)w.ldp + (unsigned)at_p) * 2u;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(P_LISTED ? p_rsrc : p_here,
+            const int rp = opaque(row_p), rq0 = opaque(row_q);  // (offsets kept across the steps would not leave the registers)
+            if (rp < left && at_p < w.M)
+                off = ((unsigned)(P_LISTED ? list[(unsigned)rp] : rp) * (unsigned)w.ldp + (unsigned)at_p) * 2u;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(P_LISTED ? p_rsrc : here,
                                                      (__attribute__((address_space(3))) void*)(to + wave * 1024), 16, off, 0, 0, 0);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int rq = kt * kGradRows + row_q + 8 * i;
+                const int rq = rq0 + 8 * i;
                 off = kPast;
-                if (rq < rows && at_q < w.N)
-                    off = ((unsigned)(P_LISTED ? rq : w.rows[first + rq]) * (unsigned)w.ldq + (unsigned)at_q) * 2u;
+                if (rq < left && at_q < w.N)
+                    off = ((unsigned)(P_LISTED ? rq : list[(unsigned)rq]) * (unsigned)w.ldq + (unsigned)at_q) * 2u;
                 __builtin_amdgcn_raw_ptr_buffer_load_lds(
-                    P_LISTED ? q_here : q_rsrc,
+                    P_LISTED ? here : q_rsrc,
                     (__attribute__((address_space(3))) void*)(to + kFewPanelM + (wave + 4 * i) * 1024), 16, off, 0, 0, 0);
             }
         };
