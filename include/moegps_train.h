@@ -79,7 +79,8 @@ int moe_combine_backward(const void* dout, int dtype, int T, int d, int k, int E
  *              wanted.  dW3 is NULL with relu
  * bf16: sums in fp32; h, da and db are rounded to bf16 as operands of the next products, results once.  The result does
  * not depend on the order in which parts of the launch run.  Outputs and workspace overlap nothing.
- * bf16 needs d % 64 == 0 and T*k*d < 2^31, f32 d % 4 == 0 and ffn % 4 == 0; limits otherwise as in the forward pass.
+ * bf16 needs d % 64 == 0 and T*k*d < 2^31, and for dx_perm ffn <= 2^21 (relu: below 2^22), f32 d % 4 == 0 and ffn % 4 == 0;
+ * limits otherwise as in the forward pass.
  * T = 0 writes zeros to the weight gradients.  Arguments are checked before the first launch.
  *
  * moe_pack_weights_backward lays the weights out for the products with transposed weights, like moe_pack_weights whenever they have

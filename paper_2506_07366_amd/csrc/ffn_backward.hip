@@ -472,6 +472,8 @@ extern "C" int moe_grouped_ffn_backward(const moe_ffn_backward_args* args, void*
     const bool bf16 = a.dtype == MOE_DTYPE_BF16;
     if (bf16 ? a.d % 64 != 0 : a.d % 4 != 0 || a.ffn % 4 != 0) return MOE_ERR_UNSUPPORTED;
     if ((int64_t)256 * (a.d > a.ffn + 63 ? a.d : a.ffn + 63) * 2 >= (1ll << 31)) return MOE_ERR_UNSUPPORTED;  // 32-bit tile offsets
+    // the product for dx sums over da's and db's columns: no more of them than the widest matrix has (a panel's 32-bit offsets)
+    if (bf16 && a.dx_perm && (int64_t)(a.relu ? 1 : 2) * padded_ffn(a.ffn, a.dtype) > kMaxWidth) return MOE_ERR_UNSUPPORTED;
     const int64_t A = (int64_t)a.T * a.k;
     if (bf16 && A * a.d >= (1ll << 31)) return MOE_ERR_UNSUPPORTED;  // 32-bit row offsets
     if (!a.packed || (bf16 && !a.packed_backward) || !a.workspace) return MOE_ERR_INVALID_ARG;

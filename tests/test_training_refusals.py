@@ -35,3 +35,16 @@ def test_packed_weights_into_a_buffer_of_another_size(form):
         pack(gpu(size()))
     with pytest.raises(B.MoeGpsError, match="out must be a GPU tensor"):
         pack(torch.zeros(size(), dtype=torch.uint8))
+
+
+def test_widths_whose_dx_sums_over_more_than_a_panel():
+    """dx is a sum over the columns of da and db, 2^22 at most; the gradients of the weights are not concerned."""
+    from test_train_host import UNSUPPORTED, ffn_backward
+    WORKSPACE = -3  # all else is in order
+    relu = dict(relu=1, dW3=0)
+    assert ffn_backward(ffn=2**21) == WORKSPACE
+    for ffn in (2**21 + 1, 2**21 + 64, 3 * 2**20, 2**22 - 64):
+        assert ffn_backward(ffn=ffn) == UNSUPPORTED, ffn
+        assert ffn_backward(ffn=ffn, dx=0) == WORKSPACE, ffn
+        assert ffn_backward(ffn=ffn, **relu) == WORKSPACE, ffn
+        assert ffn_backward(ffn=ffn, dtype=0) == (WORKSPACE if ffn % 4 == 0 else UNSUPPORTED), ffn
