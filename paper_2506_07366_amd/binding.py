@@ -550,6 +550,16 @@ def moe_grouped_ffn_backward_workspace_bytes(T: int, k: int, d: int, ffn: int, E
     return int(load_library().moe_grouped_ffn_backward_workspace_bytes(T, k, d, ffn, E, nseg, dtype, relu))
 
 
+def _need_packed(packed: Optional[torch.Tensor], n: int, name: str) -> None:
+    """Packed weights of n bytes: a kernel reads as many as the shape and the form have.  n = 0: none is read, or the library
+    refuses the shape."""
+    if n == 0:
+        return
+    size = _need(packed, packed.dtype, name).numel() * packed.element_size()
+    if size != n:
+        raise MoeGpsError(f"{name} must be the {n} bytes of these weights, got {size}")
+
+
 # moe_ffn_backward_args: eight int32, then pointers and a size of eight bytes
 _FFN_BACKWARD_ARGS = struct.Struct("@8i14Q")
 
@@ -581,16 +591,21 @@ def moe_grouped_ffn_backward(x, assign_of_row: torch.Tensor, k: int, dy_perm: to
     if out is None:
         out = tuple(None if relu and name == "dW3" else torch.empty(shape, dtype=dy_perm.dtype, device=dy_perm.device)
                     for name, shape in shapes)
+    if len(out) != len(shapes):
+        raise MoeGpsError("out must be (dx_perm, dW1, dW3, dW2)")
     for t, (name, shape) in zip(out, shapes):
         if t is not None:
             _need_shape(_need(t, dy_perm.dtype, name), shape, name)
+    _need_packed(packed, (lib.moe_packed_weights_relu_bytes if relu else lib.moe_packed_weights_bytes)(E, d, ffn, dt), "packed")
+    _need_packed(packed_backward, lib.moe_packed_weights_backward_bytes(E, d, ffn, dt, relu), "packed_backward")
     if workspace is None:
         workspace = torch.empty(moe_grouped_ffn_backward_workspace_bytes(T, k, d, ffn, E, nseg, dt, relu),
                                 dtype=torch.uint8, device=dy_perm.device)
+    _need(workspace, workspace.dtype, "workspace")
     p = _ptr
     args = _FFN_BACKWARD_ARGS.pack(
         dt, T, k, d, ffn, E, nseg, relu, p(x), p(scales) or 0, p(assign_of_row), p(seg_offsets), p(slot_expert), p(packed),
-        p(packed_backward), p(dy_perm), *(p(t) or 0 for t in out), p(workspace), workspace.numel())
+        p(packed_backward) or 0, p(dy_perm), *(p(t) or 0 for t in out), p(workspace), workspace.numel())
     _check(lib.moe_grouped_ffn_backward(args, _stream()), "moe_grouped_ffn_backward")
     return tuple(out)
 
