@@ -516,6 +516,8 @@ def moe_combine_backward(dout: torch.Tensor, y_perm, row_of_assign: torch.Tensor
     if dw is not None:
         _need_shape(_need(dw, torch.float32, "dtopk_w"), (T, k), "dtopk_w")
     if dl is not None:
+        if E < 1 and T > 0:
+            raise MoeGpsError("E, the number of experts, goes with topk_idx")
         _need_shape(_need(dl, torch.float32, "dlogits"), (T, E), "dlogits")
     _check(lib.moe_combine_backward(_ptr(dout), dt, T, d, k, E, _ptr(row_of_assign), _ptr(topk_w), _ptr(topk_idx),
                                     _ptr(y_perm), _ptr(scales), _ptr(dy), _ptr(dw), _ptr(dl), _stream()),

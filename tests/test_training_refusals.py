@@ -55,6 +55,16 @@ def test_widths_whose_dx_sums_over_more_than_a_panel():
         assert ffn_backward(ffn=ffn, dtype=0) == (WORKSPACE if ffn % 4 == 0 else UNSUPPORTED), ffn
 
 
+def test_router_gradient_without_the_number_of_experts():
+    """E belongs to topk_idx: without it there was an empty dlogits."""
+    T, k = 4, 2
+    args = (gpu(T, 64), gpu(T * k, 64), gpu(T * k, dtype=torch.int32), gpu(T, k, dtype=torch.float32))
+    idx = gpu(T, k, dtype=torch.int32)
+    with pytest.raises(B.MoeGpsError, match="E, the number of experts"):
+        B.moe_combine_backward(*args, topk_idx=idx, out=(gpu(T * k, 64), gpu(T, k, dtype=torch.float32),
+                                                         gpu(T, 0, dtype=torch.float32)))
+
+
 def ffn_backward_call(dtype=torch.bfloat16, relu=False, **kw):
     T, k = 4, 2
     code = 1 if dtype == torch.bfloat16 else 0
