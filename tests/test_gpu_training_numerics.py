@@ -1,5 +1,6 @@
 """What is kept in which precision on the way to the gradients."""
 import numpy as np
+import numpy as np
 import pytest
 import torch
 
