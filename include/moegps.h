@@ -302,7 +302,7 @@ int moe_grouped_ffn_set_option(int option, int value);
 /*
  * The ReLU form of the expert FFN (Discussion, "Generality across model architectures":
  * Switch Transformer uses ReLU in its FFN, with top-1 routing):
- *     y_perm[r] = max(x_perm[r] W1_e, 0) W2_e        no gate matrix, no biases
+ *     y_perm[r] = max(x_perm[r] W1_e, 0) W2_e        no gate matrix, no biases; max(NaN, 0) is 0
  * moe_pack_weights_relu repacks W1 [E, d, ffn] and W2 [E, ffn, d] into
  * moe_packed_weights_relu_bytes(E, d, ffn, dtype) bytes; moe_grouped_ffn_relu takes the
  * arguments of moe_grouped_ffn (same workspace size, same limits, same precision rules:

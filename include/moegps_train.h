@@ -77,6 +77,8 @@ int moe_combine_backward(const void* dout, int dtype, int T, int d, int k, int E
  *   dx_perm    [T*k, d] dtype out, rows of segments whose slot holds no expert are not written; NULL: not wanted
  *   dW1, dW3 [E, d, ffn], dW2 [E, ffn, d] dtype out, written whole (zeros for experts without rows); NULL, all of them: not
  *              wanted.  dW3 is NULL with relu
+ * Infinities and NaN reach dx_perm of the rows that have them and the weight gradients of these rows' experts, nothing else;
+ * with relu a sum a that is NaN counts as 0 (h = da = 0), as in the forward pass.
  * bf16: sums in fp32; h, da and db are rounded to bf16 as operands of the next products, results once.  The result does
  * not depend on the order in which parts of the launch run.  Outputs and workspace overlap nothing.
  * bf16 needs d % 64 == 0 and T*k*d < 2^31, and for dx_perm ffn <= 2^21 (relu: below 2^22), f32 d % 4 == 0 and ffn % 4 == 0;

@@ -1,12 +1,11 @@
-"""What is kept in which precision on the way to the gradients."""
-import numpy as np
+"""What is kept in which precision on the way to the gradients, and where values that are not finite go."""
 import numpy as np
 import pytest
 import torch
 
 from paper_2506_07366_amd import binding as B
 from gpu_util import dev_i32
-from test_gpu_training import DT
+from test_gpu_training import DT, ffn_case, run_ffn
 
 pytestmark = pytest.mark.gpu
 
@@ -32,3 +31,54 @@ def test_gradient_of_the_hidden_activation_is_not_rounded(dtype, E):
     assert torch.all(dW1[0, n:] == 0) and torch.all(dW3[0, n:] == 0)
     assert torch.all(dx == dxv)
     assert torch.all(dW2[0, :, 0] == n * 144 * 256) and torch.all(dW2[0, :, 1] == n * 144) and torch.all(dW2[0, :, 2:] == 0)
+
+
+def case_with(bad, where, dtype, relu, rows=(40, 30, 9)):
+    """Three experts; one value of row 3 (expert 0), of its input or of its result's gradient, is not finite."""
+    c = ffn_case(list(rows), [0, 1, 2], 3, 1, 128, 72, dtype, relu, seed=17)
+    clean = run_ffn(c)
+    row, at = 3, 17
+    token = int(c["assign"][row])
+    if where == "x":
+        c["x"][token, at] = bad
+    else:
+        c["dy"][row, at] = bad
+    return c, clean, run_ffn(c), row, at
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("where", ["x", "dy"])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("rows", [(40, 30, 9), (40, 30, 70)])  # small tiles, large ones
+def test_values_that_are_not_finite_stay_with_their_row_and_expert(dtype, where, bad, rows):
+    c, clean, got, row, at = case_with(bad, where, dtype, False, rows)
+    dx, dW1, dW3, dW2 = got
+    others = torch.arange(dx.shape[0], device="cuda") != row
+    assert torch.equal(dx[others], clean[0][others]) and not torch.isfinite(dx[row]).any()
+    for g, before in zip(got[1:], clean[1:]):
+        assert torch.equal(g[1:], before[1:])
+    if where == "dy":  # h is as it was: one column of dW2 has it
+        assert not torch.isfinite(dW2[0][:, at]).any()
+        keep = torch.arange(dW2.shape[2], device="cuda") != at
+        assert torch.equal(dW2[0][:, keep], clean[3][0][:, keep])
+    else:
+        assert not torch.isfinite(dW2[0]).any()
+    assert not torch.isfinite(dW1[0]).any() and not torch.isfinite(dW3[0]).any()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_nan_sums_under_relu_count_as_zero(dtype):
+    """As in the forward pass, max(a, 0) of a that is not a number is 0: the row adds nothing, but for its own NaN times 0."""
+    c, clean, got, row, at = case_with(float("nan"), "x", dtype, True)
+    dx, dW1, _, dW2 = got
+    assert torch.all(dx[row] == 0)
+    others = torch.arange(dx.shape[0], device="cuda") != row
+    assert torch.equal(dx[others], clean[0][others])
+    assert torch.isnan(dW1[0][at]).all()
+    keep = torch.arange(dW1.shape[1], device="cuda") != at
+    assert torch.isfinite(dW1[0][keep]).all() and torch.isfinite(dW2).all()
+    assert torch.equal(dW1[1:], clean[1][1:]) and torch.equal(dW2[1:], clean[3][1:])
+    # the forward pass of the same row: zeros
+    y = B.moe_grouped_ffn(c["x"][torch.from_numpy(c["assign"].astype(np.int64)).cuda()], dev_i32(c["seg"]), dev_i32(c["slot_expert"]),
+                          B.moe_pack_weights_relu(c["W1"], c["W2"]), 3, c["ffn"], relu=True)
+    assert torch.all(y[row] == 0)
