@@ -6,6 +6,7 @@ import torch
 from paper_2506_07366_amd import binding as B
 from gpu_util import dev_i32
 from test_gpu_training import DT, ffn_case, run_ffn
+from test_gpu_training_layer import host, make, step
 
 pytestmark = pytest.mark.gpu
 
@@ -31,6 +32,27 @@ def test_gradient_of_the_hidden_activation_is_not_rounded(dtype, E):
     assert torch.all(dW1[0, n:] == 0) and torch.all(dW3[0, n:] == 0)
     assert torch.all(dx == dxv)
     assert torch.all(dW2[0, :, 0] == n * 144 * 256) and torch.all(dW2[0, :, 1] == n * 144) and torch.all(dW2[0, :, 2:] == 0)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("act", ["swiglu", "relu"])
+def test_what_rows_kept_in_8_bits_cost(dtype, act):
+    """Gradients from rows kept in 8 bits against those from the rows themselves.  A kept value is off by half a step, 2^-4 of it,
+    at most; rounding errors are spread evenly within that and independent: their norm is u = 2^-4 / sqrt(3) of the rows' norm at
+    most.  dtopk_w and dlogits are linear in y.  dW1 and dW3 are x times what depends on a = x W1 and b = x W3, dW2 depends on both, dx
+    on da and db: three times u at most, to first order.  With ReLU an error moves a through 0 where |a| is of its size, u in
+    the norm of a unit normal: a fraction u * sqrt(2 / pi) of the terms comes or goes, sqrt(u) of the norm."""
+    c = make(600, 2, 8, 4, 3, 128, 72, dtype, act=act, mode=0, saved="plain")
+    want = {n: host(v) for n, v in step(c).items() if v is not None}
+    kept = make(600, 2, 8, 4, 3, 128, 72, dtype, act=act, mode=0, saved="8bit")
+    got = {n: host(v) for n, v in step(kept).items() if v is not None}
+    u = 2.0 ** -4 / 3 ** 0.5
+    own = 2 * 2.0 ** -8 if dtype == "bf16" else 1e-4   # both sides' own roundings
+    for n, w in want.items():
+        size = np.linalg.norm(want["dtopk_w"]) if n == "dlogits" else np.linalg.norm(w)
+        bound = u if n in ("dtopk_w", "dlogits") else 3 * u if act == "swiglu" else u + u ** 0.5
+        err = np.linalg.norm(got[n] - w) / size
+        assert err <= bound + own, (n, err)
 
 
 def case_with(bad, where, dtype, relu, rows=(40, 30, 9)):
