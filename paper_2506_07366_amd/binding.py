@@ -2,7 +2,7 @@
 
 Every function takes torch tensors that already live on the GPU, checks dtype /
 contiguity / device, passes raw device pointers and the current HIP stream to the
-C ABI declared in ``include/moegps.h`` and ``include/moegps_train.h`` and raises ``MoeGpsError`` on a non-zero
+C ABI declared in ``include/moegps.h``, ``include/moegps_train.h`` and ``include/moegps_mx4.h`` and raises ``MoeGpsError`` on a non-zero
 return code.  There is no CPU fallback: if the shared library has not been built
 the first call raises.
 """
@@ -35,6 +35,12 @@ EXPORTS = [
 EXPORTS_TRAIN = [
     "moe_checkpoint_store", "moe_checkpoint_load", "moe_combine_backward", "moe_packed_weights_backward_bytes",
     "moe_pack_weights_backward", "moe_grouped_ffn_backward_workspace_bytes", "moe_grouped_ffn_backward",
+]
+# declared in include/moegps_mx4.h
+EXPORTS_MX4 = [
+    "moe_packed_weights_mx4_bytes", "moe_pack_weights_mx4", "moe_unpack_weights_mx4", "moe_packed_matrix_mx4_bytes",
+    "moe_pack_matrix_mx4", "moe_unpack_matrix_mx4", "moe_grouped_product_mx4_workspace_bytes", "moe_grouped_product_mx4",
+    "moe_grouped_ffn_mx4_workspace_bytes", "moe_grouped_ffn_mx4", "moe_layer_step_mx4",
 ]
 
 
@@ -125,6 +131,24 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.moe_grouped_ffn_backward_workspace_bytes.argtypes = [c_int] * 8
     lib.moe_grouped_ffn_backward.restype = c_int
     lib.moe_grouped_ffn_backward.argtypes = [ctypes.c_char_p, vp]
+    lib.moe_packed_weights_mx4_bytes.restype = c_sz
+    lib.moe_packed_weights_mx4_bytes.argtypes = [c_int] * 4
+    lib.moe_pack_weights_mx4.restype = c_int
+    lib.moe_pack_weights_mx4.argtypes = [vp, vp, vp, c_int, c_int, c_int, c_int, vp, vp]
+    lib.moe_unpack_weights_mx4.restype = c_int
+    lib.moe_unpack_weights_mx4.argtypes = [vp, c_int, c_int, c_int, c_int, vp, vp, vp, c_int, vp]
+    lib.moe_packed_matrix_mx4_bytes.restype = c_sz
+    lib.moe_packed_matrix_mx4_bytes.argtypes = [c_int] * 3
+    lib.moe_pack_matrix_mx4.restype = c_int
+    lib.moe_pack_matrix_mx4.argtypes = [vp, c_int, c_int, c_int, c_int, vp, vp]
+    lib.moe_unpack_matrix_mx4.restype = c_int
+    lib.moe_unpack_matrix_mx4.argtypes = [vp, c_int, c_int, c_int, vp, c_int, vp]
+    for call in (lib.moe_grouped_product_mx4_workspace_bytes, lib.moe_grouped_ffn_mx4_workspace_bytes):
+        call.restype = c_sz
+        call.argtypes = [c_i64] + [c_int] * 4
+    for call in (lib.moe_grouped_product_mx4, lib.moe_grouped_ffn_mx4, lib.moe_layer_step_mx4):
+        call.restype = c_int
+        call.argtypes = [ctypes.c_char_p, vp]
     if path is None:
         _lib = lib
     return lib
@@ -278,9 +302,9 @@ _STEP_ARGS = struct.Struct("@12i24Q")
 def moe_layer_step(mode, dtype, T, d, ffn, E, k, G, S, c_max, relu, gate_in_ffn, *, logits, x, hist_pred, pred_idx,
                    packed, topk_idx, topk_w, hist, hist_plan, slot_expert, slot_quota, rank_load_pred, n_iters,
                    seg_offsets, row_of_assign, assign_of_row, x_perm, rank_load, y_perm, out, workspace_perm,
-                   workspace_ffn) -> None:
+                   workspace_ffn, mx4=False) -> None:
     """One step of the layer in one call; tensors as the single calls take them (``x_perm`` None: the FFN
-    gathers the token rows)."""
+    gathers the token rows).  ``mx4``: moe_layer_step_mx4, weights from moe_pack_weights_mx4."""
     for t in (hist_pred, pred_idx):
         if t is not None:
             _need(t, torch.int32, "hist_pred / pred_idx")
@@ -300,6 +324,10 @@ def moe_layer_step(mode, dtype, T, d, ffn, E, k, G, S, c_max, relu, gate_in_ffn,
         p(rank_load_pred), p(n_iters), p(seg_offsets), p(row_of_assign), p(assign_of_row), p(x_perm) or 0,
         p(rank_load), p(y_perm), p(out), p(workspace_perm), workspace_perm.numel(), p(workspace_ffn),
         workspace_ffn.numel())
+    if mx4:
+        _need_packed(packed, moe_packed_weights_mx4_bytes(E, d, ffn, relu), "packed")
+        _check(load_library().moe_layer_step_mx4(args, _stream()), "moe_layer_step_mx4")
+        return
     _check(load_library().moe_layer_step(args, _stream()), "moe_layer_step")
 
 
@@ -610,6 +638,172 @@ def moe_grouped_ffn_backward(x, assign_of_row: torch.Tensor, k: int, dy_perm: to
         p(packed_backward) or 0, p(dy_perm), *(p(t) or 0 for t in out), p(workspace), workspace.numel())
     _check(lib.moe_grouped_ffn_backward(args, _stream()), "moe_grouped_ffn_backward")
     return tuple(out)
+
+
+MX4_GROUP = 32  # weights that share a scale
+
+
+def moe_packed_weights_mx4_bytes(E: int, d: int, ffn: int, relu: bool = False) -> int:
+    return int(load_library().moe_packed_weights_mx4_bytes(E, d, ffn, relu))
+
+
+def moe_pack_weights_mx4(W1: torch.Tensor, W3: Optional[torch.Tensor], W2: torch.Tensor,
+                         out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Expert weights (W1, W3 [E, d, ffn], W2 [E, ffn, d]; W3 None: the ReLU form) in 4 bits, laid out for
+    moe_grouped_ffn_mx4.  ``out``: optional buffer of moe_packed_weights_mx4_bytes to write into."""
+    lib = load_library()
+    dt = dtype_code(W1)
+    for name, t in (("W1", W1), ("W3", W3), ("W2", W2)):
+        if t is not None:
+            _need(t, W1.dtype, name)
+    E, d, ffn = W1.shape
+    if (W3 is not None and tuple(W3.shape) != (E, d, ffn)) or tuple(W2.shape) != (E, ffn, d):
+        raise MoeGpsError("weight shapes must be W1,W3 [E,d,ffn] and W2 [E,ffn,d]")
+    packed = _room(out, moe_packed_weights_mx4_bytes(E, d, ffn, W3 is None), W1.device)
+    _need_one_device(W1, W3, W2, packed)
+    _check(lib.moe_pack_weights_mx4(_ptr(W1), _ptr(W3), _ptr(W2), dt, E, d, ffn, _ptr(packed), _stream()),
+           "moe_pack_weights_mx4")
+    return packed
+
+
+def moe_unpack_weights_mx4(packed: torch.Tensor, E: int, d: int, ffn: int, dtype: torch.dtype, relu: bool = False, out=None):
+    """(W1, W3, W2): the values that packed weights stand for (W3 None with ``relu``).  ``out``: optional (W1, W3, W2) to
+    write into; None among them: not wanted."""
+    lib = load_library()
+    _need_packed(packed, moe_packed_weights_mx4_bytes(E, d, ffn, relu), "packed")
+    shapes = (("W1", (E, d, ffn)), ("W3", (E, d, ffn)), ("W2", (E, ffn, d)))
+    if out is None:
+        out = tuple(None if relu and name == "W3" else torch.empty(shape, dtype=dtype, device=packed.device)
+                    for name, shape in shapes)
+    if len(out) != len(shapes):
+        raise MoeGpsError("out must be (W1, W3, W2)")
+    for t, (name, shape) in zip(out, shapes):
+        if t is not None:
+            _need_shape(_need(t, dtype, name), shape, name)
+    _need_one_device(packed, *out)
+    code = dtype_code(torch.empty(0, dtype=dtype))
+    _check(lib.moe_unpack_weights_mx4(_ptr(packed), E, d, ffn, relu, *(_ptr(t) for t in out), code, _stream()),
+           "moe_unpack_weights_mx4")
+    return tuple(out)
+
+
+def moe_packed_matrix_mx4_bytes(E: int, K: int, N: int) -> int:
+    return int(load_library().moe_packed_matrix_mx4_bytes(E, K, N))
+
+
+def moe_pack_matrix_mx4(W: torch.Tensor, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """One matrix per expert, W [E, K, N], in 4 bits, laid out for moe_grouped_product_mx4."""
+    lib = load_library()
+    dt = dtype_code(W)
+    _need(W, W.dtype, "W")
+    E, K, N = W.shape
+    packed = _room(out, moe_packed_matrix_mx4_bytes(E, K, N), W.device)
+    _need_one_device(W, packed)
+    _check(lib.moe_pack_matrix_mx4(_ptr(W), dt, E, K, N, _ptr(packed), _stream()), "moe_pack_matrix_mx4")
+    return packed
+
+
+def moe_unpack_matrix_mx4(packed: torch.Tensor, E: int, K: int, N: int, dtype: torch.dtype,
+                          out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The values [E, K, N] that a packed matrix stands for."""
+    lib = load_library()
+    _need_packed(packed, moe_packed_matrix_mx4_bytes(E, K, N), "packed")
+    if out is None:
+        out = torch.empty((E, K, N), dtype=dtype, device=packed.device)
+    _need_shape(_need(out, dtype, "out"), (E, K, N), "out")
+    _need_one_device(packed, out)
+    _check(lib.moe_unpack_matrix_mx4(_ptr(packed), E, K, N, _ptr(out), dtype_code(out), _stream()), "moe_unpack_matrix_mx4")
+    return out
+
+
+def moe_grouped_product_mx4_workspace_bytes(A: int, K: int, N: int, nseg: int, dtype: int) -> int:
+    return int(load_library().moe_grouped_product_mx4_workspace_bytes(A, K, N, nseg, dtype))
+
+
+def moe_grouped_ffn_mx4_workspace_bytes(A: int, d: int, ffn: int, nseg: int, dtype: int) -> int:
+    return int(load_library().moe_grouped_ffn_mx4_workspace_bytes(A, d, ffn, nseg, dtype))
+
+
+def _need_one_device(*tensors: Optional[torch.Tensor]) -> None:
+    """All on the current device, whose stream the call goes to."""
+    device = next(t for t in tensors if t is not None).device
+    if any(t is not None and t.device != device for t in tensors):
+        raise MoeGpsError("tensors must be on one device")
+    if device.index is not None and device.index != torch.cuda.current_device():
+        raise MoeGpsError(f"tensors are on {device}, the current device is {torch.cuda.current_device()}")
+
+
+# moe_product_mx4_args and moe_ffn_mx4_args: eight or ten int32, then numbers, pointers and a size of eight bytes
+_PRODUCT_MX4_ARGS = struct.Struct("@8i2q8QQ")
+_FFN_MX4_ARGS = struct.Struct("@10i2q8QQ")
+
+
+def _rows_mx4(x: torch.Tensor, seg_offsets: torch.Tensor, slot_expert: torch.Tensor, width: int, seg_begin: int,
+              seg_end: Optional[int], assign_of_row: Optional[torch.Tensor], k: int, topk_w: Optional[torch.Tensor],
+              out: Optional[torch.Tensor]):
+    """What both calls say about their rows: (dtype, A, rows of x, nseg, seg_end, k, out)."""
+    dt = dtype_code(x)
+    _need(x, x.dtype, "x")
+    rows = x.shape[0]
+    nseg = _need(slot_expert, torch.int32, "slot_expert").numel()
+    if _need(seg_offsets, torch.int32, "seg_offsets").numel() != nseg + 1:
+        raise MoeGpsError("seg_offsets must have one entry more than slot_expert")
+    A = rows
+    if assign_of_row is not None:
+        A = _need(assign_of_row, torch.int32, "assign_of_row").numel()
+        if k < 1 or A != rows * k:
+            raise MoeGpsError("assign_of_row must have k entries per row of x")
+    if topk_w is not None:
+        if assign_of_row is None:
+            raise MoeGpsError("topk_w goes with assign_of_row")
+        if _need(topk_w, torch.float32, "topk_w").numel() != A:
+            raise MoeGpsError("topk_w must have one entry per assignment")
+    if out is None:
+        out = torch.zeros((A, width), dtype=x.dtype, device=x.device)
+    _need_shape(_need(out, x.dtype, "out"), (A, width), "out")
+    return dt, A, rows, nseg, nseg if seg_end is None else seg_end, k, out
+
+
+def moe_grouped_product_mx4(x: torch.Tensor, seg_offsets: torch.Tensor, slot_expert: torch.Tensor, packed: torch.Tensor, E: int,
+                            N: int, assign_of_row: Optional[torch.Tensor] = None, k: int = 1,
+                            topk_w: Optional[torch.Tensor] = None, seg_begin: int = 0, seg_end: Optional[int] = None,
+                            workspace: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """y [A, N]: every row times its expert's matrix (``packed`` from moe_pack_matrix_mx4).  ``x``: permuted rows [A, K], or
+    with ``assign_of_row`` the tokens' rows [A / k, K].  ``topk_w``: gate weights that the results are multiplied by."""
+    dt, A, rows, nseg, seg_end, k, out = _rows_mx4(x, seg_offsets, slot_expert, N, seg_begin, seg_end, assign_of_row, k, topk_w,
+                                                   out)
+    K = x.shape[1]
+    _need_packed(packed, moe_packed_matrix_mx4_bytes(E, K, N), "packed")
+    if workspace is None:
+        workspace = torch.empty(moe_grouped_product_mx4_workspace_bytes(A, K, N, nseg, dt), dtype=torch.uint8, device=x.device)
+    _need(workspace, torch.uint8, "workspace")
+    _need_one_device(x, assign_of_row, seg_offsets, slot_expert, topk_w, packed, out, workspace)
+    p = _ptr
+    args = _PRODUCT_MX4_ARGS.pack(dt, K, N, E, nseg, seg_begin, seg_end, k, A, rows, p(x), p(assign_of_row) or 0, p(seg_offsets),
+                                  p(slot_expert), p(topk_w) or 0, p(packed), p(out), p(workspace), workspace.numel())
+    _check(load_library().moe_grouped_product_mx4(args, _stream()), "moe_grouped_product_mx4")
+    return out
+
+
+def moe_grouped_ffn_mx4(x: torch.Tensor, seg_offsets: torch.Tensor, slot_expert: torch.Tensor, packed: torch.Tensor, E: int,
+                        ffn: int, relu: bool = False, assign_of_row: Optional[torch.Tensor] = None, k: int = 1,
+                        topk_w: Optional[torch.Tensor] = None, seg_begin: int = 0, seg_end: Optional[int] = None,
+                        workspace: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """y [A, d]: the experts' FFN with weights in 4 bits (``packed`` from moe_pack_weights_mx4).  ``x``: permuted rows
+    [A, d], or with ``assign_of_row`` the tokens' rows [A / k, d].  ``topk_w``: gate weights that the results are multiplied by."""
+    d = x.shape[1]
+    dt, A, rows, nseg, seg_end, k, out = _rows_mx4(x, seg_offsets, slot_expert, d, seg_begin, seg_end, assign_of_row, k, topk_w,
+                                                   out)
+    _need_packed(packed, moe_packed_weights_mx4_bytes(E, d, ffn, relu), "packed")
+    if workspace is None:
+        workspace = torch.empty(moe_grouped_ffn_mx4_workspace_bytes(A, d, ffn, nseg, dt), dtype=torch.uint8, device=x.device)
+    _need(workspace, torch.uint8, "workspace")
+    _need_one_device(x, assign_of_row, seg_offsets, slot_expert, topk_w, packed, out, workspace)
+    p = _ptr
+    args = _FFN_MX4_ARGS.pack(dt, d, ffn, E, nseg, seg_begin, seg_end, k, relu, 0, A, rows, p(x), p(assign_of_row) or 0,
+                              p(seg_offsets), p(slot_expert), p(topk_w) or 0, p(packed), p(out), p(workspace), workspace.numel())
+    _check(load_library().moe_grouped_ffn_mx4(args, _stream()), "moe_grouped_ffn_mx4")
+    return out
 
 
 def moe_comm_matrix(mode: int, topk_idx: torch.Tensor, pred_idx: Optional[torch.Tensor],

@@ -14,6 +14,7 @@
 // Whole steps, us, six calls (seven with predicted ids) -> one: 256 tokens of the small fp32 layer 45.0 -> 39.9 (no
 // longer bound by the host, which takes 22), one token on 128 experts 80.2 -> 74.9, 777 tokens with Token-to-Expert 438 ->
 // 427; batches of some 300 us and more gain less than the runs differ.
+#include "mx4.h"
 #include "permute.h"
 #include "plan_regs.h"
 #include "route_tokens.h"
@@ -106,10 +107,8 @@ static int route_and_plan(const PlanJob& p, const float* logits, int T, int k, i
     }
 }
 
-}  // namespace moegps
-
-extern "C" int moe_layer_step(const moe_layer_step_args* a, void* stream) {
-    using namespace moegps;
+// mx4: the experts' weights are in 4 bits (mx4.hip), and the rows are gathered in any form of the FFN
+static int layer_step(const moe_layer_step_args* a, bool mx4, void* stream) {
     if (!a) return MOE_ERR_INVALID_ARG;
     const int mode = a->mode, T = a->T, E = a->E, k = a->k, G = a->G, S = a->S;
     // what the calls of the single steps would refuse, before the first launch
@@ -122,7 +121,8 @@ extern "C" int moe_layer_step(const moe_layer_step_args* a, void* stream) {
     if (ceil_div(E, G) > S) return MOE_ERR_INVALID_ARG;
     if ((int64_t)T * k >= (1ll << 31) || route_blocks(T, E) >= kRouteMaxBlocks) return MOE_ERR_UNSUPPORTED;
     if (((size_t)a->d * dtype_size(a->dtype)) % 16 != 0) return MOE_ERR_UNSUPPORTED;
-    if (a->relu && !a->x_perm) return MOE_ERR_UNSUPPORTED;  // the row gather is built for the SwiGLU form only
+    // with bf16 and fp32 weights the row gather is built for the SwiGLU form only
+    if (mx4 ? a->x_perm != nullptr : a->relu && !a->x_perm) return MOE_ERR_UNSUPPORTED;
     if (T == 0) return MOE_OK;
     if (!a->logits || !a->x || !a->packed || !a->topk_idx || !a->topk_w || !a->hist || !a->slot_expert ||
         !a->slot_quota || !a->rank_load_pred || !a->n_iters || !a->seg_offsets || !a->row_of_assign ||
@@ -179,6 +179,12 @@ extern "C" int moe_layer_step(const moe_layer_step_args* a, void* stream) {
     int32_t* const tokens = scratch_free ? (int32_t*)a->workspace_perm : nullptr;
     const FfnOptions opt = ffn_options();  // (once: the job and the products go by the same)
     auto ffn = [&](FfnStage stage, TableJob* job) {
+        if (mx4) {
+            const moe_ffn_mx4_args f{a->dtype, a->d, a->ffn, E, G * S, 0, G * S, k, a->relu, 0, A, T, a->x, a->assign_of_row,
+                                     a->seg_offsets, a->slot_expert, gate, a->packed, a->y_perm, a->workspace_ffn,
+                                     a->workspace_ffn_bytes};
+            return mx4_ffn_call(f, st, stage, job);
+        }
         if (copy_first)
             return grouped_ffn_call(a->relu, a->x_perm, A, nullptr, 1, nullptr, nullptr, a->dtype, A, a->d, a->ffn, E,
                                     a->seg_offsets, a->slot_expert, G * S, 0, G * S, a->packed, a->y_perm, a->workspace_ffn,
@@ -228,3 +234,9 @@ extern "C" int moe_layer_step(const moe_layer_step_args* a, void* stream) {
     if ((rc = ffn(tables_too ? kFfnTablesBuilt : kFfnAll, nullptr)) != MOE_OK) return rc;
     return moe_combine(a->y_perm, a->dtype, T, a->d, k, a->row_of_assign, gate ? nullptr : a->topk_w, a->out, stream);
 }
+
+}  // namespace moegps
+
+extern "C" int moe_layer_step(const moe_layer_step_args* a, void* stream) { return moegps::layer_step(a, false, stream); }
+
+extern "C" int moe_layer_step_mx4(const moe_layer_step_args* a, void* stream) { return moegps::layer_step(a, true, stream); }

@@ -1,0 +1,135 @@
+// Grouped products and the experts' FFN with weights in 4 bits (include/moegps_mx4.h; layout: mx4.h).
+//
+// Rows are tiled by expert, as in grouped_ffn.hip: the rows of all segments of an expert are listed one after the other by the table
+// builder (ffn_tables.h) and cut into M-tiles together.
+#include "mx4.h"
+
+namespace moegps {
+
+#include "mx4_stream.h"
+
+struct Mx4Ws {
+    int32_t* rowlist;
+    MTile* tiles;
+    int32_t* counts;
+    void* h;  // hidden activations in row-list order (FFN)
+    int capacity;
+};
+
+// hidden: width of a hidden row, 0: none
+static size_t mx4_ws_layout(int64_t A, int hidden, int nseg, int dtype, char* base, Mx4Ws* ws) {
+    size_t off = 0;
+    auto take = [&](size_t bytes) {
+        void* p = base ? (void*)(base + off) : nullptr;
+        off += align_up(bytes, 256);
+        return p;
+    };
+    const int64_t A1 = A > 0 ? A : 1;
+    Mx4Ws w;
+    w.capacity = (int)(ceil_div64(A1, kMinBM) + nseg);
+    w.rowlist = (int32_t*)take((size_t)A1 * sizeof(int32_t));
+    w.tiles = (MTile*)take((size_t)w.capacity * sizeof(MTile));
+    w.counts = (int32_t*)take(256);
+    w.h = hidden ? take((size_t)A1 * hidden * dtype_size(dtype)) : nullptr;
+    if (ws) *ws = w;
+    return off;
+}
+
+template <int EPI>
+static int launch_mx4(const Mx4Product& p, int dtype, hipStream_t st) {
+    const bool f32 = dtype == MOE_DTYPE_F32;
+    const auto kern = f32 ? mx4_stream_kernel<1, 8, EPI, true> : mx4_stream_kernel<1, 8, EPI, false>;
+    hipLaunchKernelGGL(kern, dim3(4 * kGemmGrid), dim3(512), 0, st, p);
+    return check_launch();
+}
+
+// What both calls check; `inner`: the widths whose rows are addressed.
+struct Mx4Rows {
+    int dtype, E, nseg, seg_begin, seg_end, k;
+    int64_t A, rows_x;
+    const void* x;
+    const int32_t *assign_of_row, *seg_offsets, *slot_expert;
+    const float* topk_w;
+    const void *packed, *y, *workspace;
+};
+static int check_rows(const Mx4Rows& r, int K, int N, int ffn) {
+    if (r.dtype != MOE_DTYPE_F32 && r.dtype != MOE_DTYPE_BF16) return MOE_ERR_INVALID_ARG;
+    if (r.A < 0 || K < 1 || N < 1 || ffn < 1 || r.E < 1 || r.nseg < 1) return MOE_ERR_INVALID_ARG;
+    if (r.seg_begin < 0 || r.seg_end > r.nseg || r.seg_begin > r.seg_end) return MOE_ERR_INVALID_ARG;
+    if (r.assign_of_row && (r.k < 1 || r.rows_x < 0)) return MOE_ERR_INVALID_ARG;
+    if (r.topk_w && !r.assign_of_row) return MOE_ERR_INVALID_ARG;
+    if (r.nseg > MOE_MAX_SEGMENTS || r.E > MOE_MAX_EXPERTS || r.A >= (1ll << 31)) return MOE_ERR_UNSUPPORTED;
+    if (K > kMaxWidth || N > kMaxWidth || ffn > kMaxWidth) return MOE_ERR_UNSUPPORTED;
+    if ((size_t)K * dtype_size(r.dtype) % 16 != 0 || (size_t)N * dtype_size(r.dtype) % 16 != 0) return MOE_ERR_UNSUPPORTED;
+    const int64_t rows = r.assign_of_row ? r.rows_x : r.A;
+    if (rows >= (1ll << 31) || rows * K >= (1ll << 31)) return MOE_ERR_UNSUPPORTED;
+    if (!r.seg_offsets || !r.slot_expert || !r.packed || !r.workspace) return MOE_ERR_INVALID_ARG;
+    if (r.A > 0 && (!r.x || !r.y)) return MOE_ERR_INVALID_ARG;
+    return MOE_OK;
+}
+
+int mx4_ffn_call(const moe_ffn_mx4_args& a, hipStream_t st, FfnStage stage, TableJob* job_out) {
+    if (a.reserved != 0) return MOE_ERR_INVALID_ARG;
+    const Mx4Rows rows{a.dtype, a.E, a.nseg, a.seg_begin, a.seg_end, a.k, a.A, a.rows_x, a.x, a.assign_of_row,
+                       a.seg_offsets, a.slot_expert, a.topk_w, a.packed, a.y, a.workspace};
+    if (const int rc = check_rows(rows, a.d, a.d, a.ffn); rc != MOE_OK) return rc;
+    const int hidden = mx4_hidden(a.ffn);
+    Mx4Ws ws;
+    if (a.workspace_bytes < mx4_ws_layout(a.A, hidden, a.nseg, a.dtype, (char*)a.workspace, &ws)) return MOE_ERR_WORKSPACE_TOO_SMALL;
+    if (a.A == 0 || a.seg_begin == a.seg_end) {
+        if (job_out) *job_out = TableJob{};
+        return MOE_OK;
+    }
+    const TableSpec t1{ws.tiles, ws.counts, nullptr, kMx4StreamRows, ws.capacity, 0, 0, 1, 0, 0}, none{};
+    const TableJob job{a.E, a.seg_begin, a.seg_end, t1, none, RowLists{ws.rowlist, nullptr, nullptr, 1}, nullptr, 0, nullptr, nullptr};
+    if (stage == kFfnJobOnly) {
+        *job_out = job;
+        return MOE_OK;
+    }
+    if (stage == kFfnAll)
+        if (const int rc = launch_tables(a.A, a.seg_offsets, a.slot_expert, job, st); rc != MOE_OK) return rc;
+    const RowMap rm1{ws.rowlist, a.assign_of_row, a.k, nullptr, nullptr, nullptr};
+    const RowMap rm2{nullptr, nullptr, 1, ws.rowlist, a.topk_w ? a.assign_of_row : nullptr, a.topk_w};
+    const Mx4Product p1{a.x, a.d, a.d, mx4_first(a.packed, a.d, a.ffn, a.relu), ws.h, hidden, hidden, ws.tiles, ws.counts, rm1};
+    const Mx4Product p2{ws.h, hidden, hidden, mx4_second(a.packed, a.E, a.d, a.ffn, a.relu), a.y, a.d, a.d, ws.tiles, ws.counts, rm2};
+    const int rc = a.relu ? launch_mx4<kEpiRelu>(p1, a.dtype, st) : launch_mx4<kEpiSwiglu>(p1, a.dtype, st);
+    return rc != MOE_OK ? rc : launch_mx4<kEpiNone>(p2, a.dtype, st);
+}
+
+}  // namespace moegps
+
+extern "C" size_t moe_grouped_product_mx4_workspace_bytes(int64_t A, int K, int N, int nseg, int dtype) {
+    using namespace moegps;
+    if (!ffn_shape_in_range(A, K, N, nseg, dtype)) return 0;
+    return mx4_ws_layout(A, 0, nseg, dtype, nullptr, nullptr);
+}
+
+extern "C" int moe_grouped_product_mx4(const moe_product_mx4_args* a, void* stream) {
+    using namespace moegps;
+    if (!a) return MOE_ERR_INVALID_ARG;
+    const Mx4Rows rows{a->dtype, a->E, a->nseg, a->seg_begin, a->seg_end, a->k, a->A, a->rows_x, a->x, a->assign_of_row,
+                       a->seg_offsets, a->slot_expert, a->topk_w, a->packed, a->y, a->workspace};
+    if (const int rc = check_rows(rows, a->K, a->N, 1); rc != MOE_OK) return rc;
+    Mx4Ws ws;
+    if (a->workspace_bytes < mx4_ws_layout(a->A, 0, a->nseg, a->dtype, (char*)a->workspace, &ws)) return MOE_ERR_WORKSPACE_TOO_SMALL;
+    if (a->A == 0 || a->seg_begin == a->seg_end) return MOE_OK;
+    hipStream_t st = (hipStream_t)stream;
+    const TableSpec t1{ws.tiles, ws.counts, nullptr, kMx4StreamRows, ws.capacity, 0, 0, 1, 0, 0}, none{};
+    const TableJob job{a->E, a->seg_begin, a->seg_end, t1, none, RowLists{ws.rowlist, nullptr, nullptr, 1}, nullptr, 0, nullptr, nullptr};
+    if (const int rc = launch_tables(a->A, a->seg_offsets, a->slot_expert, job, st); rc != MOE_OK) return rc;
+    const RowMap rm{ws.rowlist, a->assign_of_row, a->k, ws.rowlist, a->topk_w ? a->assign_of_row : nullptr, a->topk_w};
+    const Mx4Product p{a->x, a->K, a->K, mx4_matrix(a->packed, a->K, ceil_div(a->N, kMx4N)), a->y, a->N, a->N, ws.tiles, ws.counts, rm};
+    return launch_mx4<kEpiNone>(p, a->dtype, st);
+}
+
+extern "C" size_t moe_grouped_ffn_mx4_workspace_bytes(int64_t A, int d, int ffn, int nseg, int dtype) {
+    using namespace moegps;
+    if (!ffn_shape_in_range(A, d, ffn, nseg, dtype)) return 0;
+    return mx4_ws_layout(A, mx4_hidden(ffn), nseg, dtype, nullptr, nullptr);
+}
+
+extern "C" int moe_grouped_ffn_mx4(const moe_ffn_mx4_args* a, void* stream) {
+    using namespace moegps;
+    if (!a) return MOE_ERR_INVALID_ARG;
+    return mx4_ffn_call(*a, (hipStream_t)stream, kFfnAll, nullptr);
+}

@@ -29,14 +29,20 @@ def to_device(a: np.ndarray, dtype: str, device="cuda") -> torch.Tensor:
 
 
 class MoELayer:
-    def __init__(self, cfg: MoEConfig, device="cuda", fused_gather: bool = False, fused_weights: bool = False):
+    def __init__(self, cfg: MoEConfig, device="cuda", fused_gather: bool = False, fused_weights: bool = False,
+                 weights: str = "plain"):
         """fused_gather: gather the token rows inside the first FFN product
         (moe_grouped_ffn_gather) instead of materialising x_perm in moe_permute.
         fused_weights (implies fused_gather): the second product also applies the gate weights
-        (moe_grouped_ffn_fused) and moe_combine only adds the k rows of a token."""
+        (moe_grouped_ffn_fused) and moe_combine only adds the k rows of a token.
+        weights: "plain" keeps the expert weights in the layer's type, "mx4" in 4 bits (moe_pack_weights_mx4; for serving),
+        where the token rows are always gathered."""
+        if weights not in ("plain", "mx4"):
+            raise B.MoeGpsError(f"weights must be 'plain' or 'mx4', got {weights!r}")
         self.cfg = cfg
+        self.mx4 = weights == "mx4"
         self.fused_weights = fused_weights
-        fused_gather = fused_gather or fused_weights
+        fused_gather = fused_gather or fused_weights or self.mx4
         self.fused_gather = fused_gather
         self.dev = torch.device(device)
         c = cfg
@@ -62,8 +68,8 @@ class MoELayer:
         dcode = B.MOE_DTYPE_F32 if c.dtype == "f32" else B.MOE_DTYPE_BF16
         self.ws_perm = torch.empty(max(256, B.moe_permute_workspace_bytes(c.T, c.E, c.k, c.G, c.S)),
                                    dtype=torch.uint8, device=self.dev)
-        self.ws_ffn = torch.empty(max(256, B.moe_grouped_ffn_workspace_bytes(c.A, c.d, c.ffn, c.nseg, dcode)),
-                                  dtype=torch.uint8, device=self.dev)
+        ffn_bytes = B.moe_grouped_ffn_mx4_workspace_bytes if self.mx4 else B.moe_grouped_ffn_workspace_bytes
+        self.ws_ffn = torch.empty(max(256, ffn_bytes(c.A, c.d, c.ffn, c.nseg, dcode)), dtype=torch.uint8, device=self.dev)
         self.packed: Optional[torch.Tensor] = None
         self.in_training = False   # a MoETraining stands beside this layer (training.py)
         self.packed_backward: Optional[torch.Tensor] = None  # in training: the same weights as the backward pass wants them
@@ -72,6 +78,9 @@ class MoELayer:
     def set_weights(self, W1: torch.Tensor, W3: Optional[torch.Tensor], W2: torch.Tensor) -> None:
         """One-off repack of the (static) expert weights, into a new buffer; the ReLU form has no W3.  In training, where
         they change, they are laid out for both passes and in the same buffers every time: a recorded graph reads those set last."""
+        if self.mx4:
+            self.packed = B.moe_pack_weights_mx4(W1, None if self.cfg.act == "relu" else W3, W2)
+            return
         if self.cfg.act == "relu" and self.fused_gather:
             raise B.MoeGpsError("the fused row gather is built for the SwiGLU form only")
         # (a buffer that came from elsewhere, another layer's, is not written over)
@@ -116,7 +125,12 @@ class MoELayer:
         c = self.cfg
         if self.packed is None:
             raise B.MoeGpsError("set_weights() first")
-        if self.fused_gather:
+        if self.mx4:
+            B.moe_grouped_ffn_mx4(self._x, self.perm["seg_offsets"], self.slot_expert, self.packed, c.E, c.ffn,
+                                  relu=c.act == "relu", assign_of_row=self.perm["assign_of_row"], k=c.k,
+                                  topk_w=self.topk_w if self.fused_weights else None, seg_begin=seg_begin, seg_end=seg_end,
+                                  workspace=self.ws_ffn, out=self.y_perm)
+        elif self.fused_gather:
             B.moe_grouped_ffn_gather(self._x, self.perm["assign_of_row"], c.k, self.perm["seg_offsets"],
                                      self.slot_expert, self.packed, c.E, c.ffn, seg_begin, seg_end,
                                      workspace=self.ws_ffn, out=self.y_perm,
@@ -157,7 +171,7 @@ class MoELayer:
                          rank_load_pred=self.rank_load_pred, n_iters=self.n_iters, seg_offsets=p["seg_offsets"],
                          row_of_assign=p["row_of_assign"], assign_of_row=p["assign_of_row"], x_perm=p["x_perm"],
                          rank_load=p["rank_load"], y_perm=self.y_perm, out=self.out, workspace_perm=self.ws_perm,
-                         workspace_ffn=self.ws_ffn)
+                         workspace_ffn=self.ws_ffn, mx4=self.mx4)
         self._x = x
         self._hp = {MODE_NONE: self.hist, MODE_DISTRIBUTION: hist_pred, MODE_TOKEN: self.hist_plan}[mode]
         return True

@@ -39,6 +39,8 @@ class MoETraining:
         if layer.fused_weights:
             raise B.MoeGpsError("a layer with fused_weights keeps y_perm with the gate weights applied: its gradient needs "
                                 "the rows without them")
+        if layer.mx4:
+            raise B.MoeGpsError("weights in 4 bits are not trained")
         self.layer = layer
         layer.in_training = True
         self.saved = saved
