@@ -289,7 +289,7 @@ int moe_layer_step(const moe_layer_step_args* args, void* stream);
  *   MOE_FFN_OPT_GROUP_N        N-tiles walked side by side under one run of M-tiles, 0 automatic
  *   MOE_FFN_OPT_STREAM         weight-streaming kernels for a few rows per expert: -1 automatic,
  *                              0 never, 1 / 2 their first / second form (a forced tile shape or more
- *                              than 65536 rows comes first)
+ *                              than 65536 rows comes first).  Read by the products with 4-bit weights too
  * Returns MOE_ERR_INVALID_ARG for an unknown option or a value out of range.
  */
 #define MOE_FFN_OPT_TILE1    0

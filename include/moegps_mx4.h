@@ -54,7 +54,7 @@ int moe_unpack_matrix_mx4(const void* packed, int E, int K, int N, void* W, int 
  * bf16: exact products, summed in fp32, rounded once.  fp32: the rows are taken as three bf16 parts that add up to them, whose products
  * are summed in fp32.  Sums do not depend on the order of the launch.  Infinities and NaN stay in the rows, and with weights that are NaN
  * the columns, that have them.
- * K and N times the size of dtype must be multiples of 16; A < 2^31; rows of x (A, or rows_x) times K below 2^31.
+ * K and N times the size of dtype must be multiples of 16; A < 2^31; rows of x (A, or rows_x) times K up to 2^31 - 64.
  * Outputs and workspace overlap nothing.  A = 0 is a no-op.
  */
 typedef struct moe_product_mx4_args {

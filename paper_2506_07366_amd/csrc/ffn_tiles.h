@@ -70,10 +70,23 @@ __device__ __forceinline__ void tell_rows(int32_t* left, int& expert, int rows) 
     expert = -1;
 }
 
-template <int EPI, int LINK>
+// How weights arrive.  As bf16 fragments, as they are multiplied; or in 4 bits (Mx4Weights, mx4.h), a panel per wavefront, its codes
+// and scales turned into fragments where they are multiplied.
+struct PlainWeights {
+    static constexpr bool kFour = false;
+    // (never called)
+    static __device__ size_t panel_bytes(int kt);
+    static __device__ unsigned lane_scales(int lane);
+    static __device__ unsigned codes_at(int i);
+    static __device__ unsigned scales_at(int i);
+    static __device__ bf16x8 values(unsigned codes, unsigned scales, int j);
+};
+
+template <int EPI, int LINK, class Weights = PlainWeights>
 __device__ __forceinline__ void tile_product(
     const bf16_t* A, int lda,                        // activations [rows, K]
-    const bf16_t* __restrict__ Bp, size_t b_stride,  // packed weights [E][N-tile][k-tile][kPackN x kPackK]
+    const bf16_t* __restrict__ Bp, size_t b_stride,  // packed weights [E][N-tile][k-tile][kPackN x kPackK]; in 4 bits
+                                                     //   [E][panel], b_stride in bytes
     bf16_t* C, int ldc,                              // output [rows, SWIGLU ? N/2 : N]
     const MTile* __restrict__ mtiles, const int32_t* __restrict__ counts, int32_t* __restrict__ queues,
     int N, int K, int group_n, bool past_caches, RowMap rm,
@@ -84,6 +97,7 @@ __device__ __forceinline__ void tile_product(
     const float* dhidden = nullptr,  // backward pass: [rows, SWIGLU ? N/2 : N] gradient of the hidden activation,
     bf16_t* hidden = nullptr) {      //   and out the hidden activation
     constexpr bool SWIGLU = EPI == kEpiSwiglu || EPI == kEpiSwigluGrad;
+    constexpr bool FOUR = Weights::kFour;  // a row is then lda long, which may be less than K, and N a multiple of 8
     constexpr int BN = kPackN, BK = kPackK, NW = 8;
     constexpr int ROW_BYTES = BK * 2;      // of an activation row in a stage
     constexpr int B_BYTES = BN * BK * 2;   // of a weight tile
@@ -232,9 +246,12 @@ __device__ __forceinline__ void tile_product(
         // SwiGLU a gate group and its up group, two further.
         const int grp0 = SWIGLU ? (wave >> 1) * 4 + (wave & 1) : wave * 2;
         constexpr int JB = (SWIGLU ? 2 : 1) * 2 * kFragElems * 2;  // bytes between the two
-        const unsigned char* Bw = (const unsigned char*)(Bp + (size_t)mt.expert * b_stride +
-                                                         ((size_t)nt_i * (K / BK) + mt.kt0) * (BN * BK)) +
-                                  grp0 * 2 * kFragElems * 2;
+        const unsigned char* Bw;
+        if constexpr (FOUR)  // the wavefront's panel
+            Bw = (const unsigned char*)Bp + (size_t)mt.expert * b_stride + (size_t)(nt_i * NW + wave) * Weights::panel_bytes(K / BK);
+        else
+            Bw = (const unsigned char*)(Bp + (size_t)mt.expert * b_stride + ((size_t)nt_i * (K / BK) + mt.kt0) * (BN * BK)) +
+                 grp0 * 2 * kFragElems * 2;
         // Both operands are addressed through buffer descriptors: a uniform base and a 32-bit offset per
         // lane, and a k-tile past the end is asked for out of the buffer's range, which keeps the number of
         // loads per k-tile fixed (the waits count them) and costs no memory access.  What such a load
@@ -242,7 +259,9 @@ __device__ __forceinline__ void tile_product(
         // Activations reach up to 2^32 - 144 bytes: fewer than 2^31 elements, a row is a multiple of 64.)
         constexpr unsigned kARange = 0xffffff80u, kAPast = 0xfffffff0u, kWRange = 0x80000000u, kWPast = 0xfffff000u;
         const auto a_rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)Ab, 0, (int)kARange, 0x00027000);
-        const auto w_rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)Bw, 0, (int)kWRange, 0x00027000);
+        // (a panel of 4-bit weights is all that a wavefront reads, nothing if its columns do not exist)
+        const unsigned w_range = !FOUR ? kWRange : (nt_i * NW + wave) * 32 < N ? (unsigned)Weights::panel_bytes(K / BK) : 0u;
+        const auto w_rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)Bw, 0, (int)w_range, 0x00027000);
         const unsigned lds_base = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)smem;
 
         // Accumulators hold the transposed product: the weight fragment is the MFMA's row operand and
@@ -268,16 +287,23 @@ __device__ __forceinline__ void tile_product(
         auto k_loop = [&](auto TM_tag, auto once_tag) {
             constexpr int TM = decltype(TM_tag)::value;
             constexpr int kAux = decltype(once_tag)::value ? kNonTemporal : 0;
-            constexpr int D = TM <= 8 ? 4 : 3;                          // k-tiles under way
-            constexpr int STAGE = (TM <= 8 ? 128 : 256) * ROW_BYTES;    // activation bytes of one of them
+            constexpr int D = Weights::kFour ? (TM <= 4 ? 8 : TM <= 8 ? 6 : 3) : TM <= 8 ? 4 : 3;  // k-tiles under way
+            constexpr int STAGE = (FOUR && TM <= 4 ? 64 : TM <= 8 ? 128 : 256) * ROW_BYTES;  // activation bytes of one of them
             static_assert((size_t)D * STAGE <= kStageLds, "LDS of the launch");
             constexpr int IA = (TM + 3) / 4;  // activation loads per wavefront and k-tile, 8 rows each
-            constexpr int NB = 4 + IA;        // loads per wavefront and k-tile
+            constexpr int NW_LOADS = FOUR ? 2 : 4;  // of weights
+            constexpr int NB = NW_LOADS + IA;       // loads per wavefront and k-tile
             constexpr int NF = 2 * TM;
-            constexpr int R = NF % 8 == 0 ? 8 : 4;
+            constexpr int R = NF % 8 == 0 && !(FOUR && TM > 12) ? 8 : 4;
             constexpr int H = NF - R / 2;     // the hand-over opens fragment H
             static_assert(NF % R == 0 && H >= 1, "fragment f sits in register f % R in every k-tile");
             unsigned offA[IA];
+            int a_end = KT;  // 4-bit weights: k-tiles of the entry in which this lane's piece of a row exists
+            if constexpr (FOUR) {
+                const int slot = (lane_p & 7) ^ swz(wave * 8 + (lane_p >> 3));  // (the same for all its rows)
+                const int end = ((lda >> 3) - slot + 7) / 8 - mt.kt0;
+                a_end = end < KT ? end : KT;
+            }
 #pragma unroll
             for (int i = 0; i < IA; ++i) {
                 const int p = (wave + i * NW) * 64 + lane_p;
@@ -293,20 +319,28 @@ __device__ __forceinline__ void tile_product(
             if constexpr (epi_copies(EPI))  // (behind the row list, whose wait would be for the pieces too)
                 if (copy_n > 0)
                     request_pieces(copy, copy_first, copy_n, smem + kStageLds + wave * (kCopyPieces * kCopyPieceLds));
-            bf16x8 w[D][2][2], af[R];
+            bf16x8 w[FOUR ? 1 : D][2][FOUR ? 1 : 2], af[R];
+            u32x4 codes[FOUR ? D : 1];
+            unsigned short scales[FOUR ? D : 1];
             const unsigned lane_off = (unsigned)(lane_p * 16);
             // load l of this wavefront's NB loads of k-tile kt, into buffers b
             auto load_n = [&](auto L, int kt, auto Bt) {
                 constexpr int l = decltype(L)::value, b = decltype(Bt)::value;
                 const bool in = kt < KT;
-                if constexpr (l < 4) {
+                if constexpr (FOUR && l == 0) {
+                    const unsigned off = lane_off + (in ? Weights::codes_at(mt.kt0 + kt) : kWPast);
+                    codes[b] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(w_rsrc, off, 0, kAux));
+                } else if constexpr (FOUR && l == 1) {
+                    const unsigned off = Weights::lane_scales(opaque(lane_p)) + (in ? Weights::scales_at(mt.kt0 + kt) : kWPast);
+                    scales[b] = __builtin_amdgcn_raw_buffer_load_b16(w_rsrc, off, 0, kAux);
+                } else if constexpr (l < NW_LOADS) {
                     constexpr int j = l >> 1, ks = l & 1;
                     const unsigned off = in ? lane_off + (unsigned)kt * B_BYTES : kWPast;
                     w[b][j][ks] = __builtin_bit_cast(
                         bf16x8, __builtin_amdgcn_raw_buffer_load_b128(w_rsrc, off + ks * kFragElems * 2, j * JB, kAux));
                 } else {
-                    constexpr int i = l - 4;
-                    const unsigned off = in ? offA[i] + (unsigned)kt * ROW_BYTES : kAPast;
+                    constexpr int i = l - NW_LOADS;
+                    const unsigned off = (FOUR ? kt < a_end : in) ? offA[i] + (unsigned)kt * ROW_BYTES : kAPast;
                     __builtin_amdgcn_raw_ptr_buffer_load_lds(
                         a_rsrc,
                         (__attribute__((address_space(3))) void*)(smem + b * STAGE + (wave + i * NW) * 1024), 16,
@@ -327,7 +361,7 @@ __device__ __forceinline__ void tile_product(
             unsigned a_lane[2][2];    // [step][lower 64 KiB of the stages, upper]: the read's offset field holds 16 bits
 #pragma unroll
             for (int ks = 0; ks < 2; ++ks) {
-                a_lane[ks][0] = lds_base + (unsigned)(l16 * ROW_BYTES + (((ks * 4 + g16) ^ sw) * 16));
+                a_lane[ks][0] = lds_base + (unsigned)(l16 * ROW_BYTES + (((FOUR ? g16 * 2 + ks : ks * 4 + g16) ^ sw) * 16));
                 a_lane[ks][1] = a_lane[ks][0] + 0x10000;
             }
             auto read_frag = [&](auto F, auto Bt) {
@@ -361,10 +395,14 @@ __device__ __forceinline__ void tile_product(
                         lds_wait<(f <= NF - R ? R - 1 : NF - 1 - f)>();  // fragment f has landed
                     }
                     lds_landed(af[f % R]);
+                    if constexpr (FOUR && i == 0)
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) w[0][j][0] = Weights::values(codes[u][2 * ks + j], scales[u], j);
                     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                     for (int j = 0; j < 2; ++j)
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[u][j][ks], af[f % R], acc[i][j], 0, 0, 0);
+                        acc[i][j] =
+                            __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[FOUR ? 0 : u][j][FOUR ? 0 : ks], af[f % R], acc[i][j], 0, 0, 0);
                     __builtin_amdgcn_sched_barrier(0);
                     if constexpr (f + R < NF) read_frag(std::integral_constant<int, f + R>{}, U);
                     else if constexpr (f >= H) read_frag(std::integral_constant<int, f - H + R / 2>{}, next);
@@ -522,7 +560,7 @@ __device__ __forceinline__ void tile_product(
                 }
             }
         } else {
-            const int col0 = n0 + wave * 32;  // (N is a multiple of 64: the wavefront's columns exist or not together)
+            const int col0 = n0 + wave * 32;  // (plain weights: N is a multiple of 64, the wavefront's columns exist or not together)
             float* slab = nullptr;
             if constexpr (EPI == kEpiNone && LINK == kAlone)
                 if (mt.part >= 0) slab = partials + (size_t)mt.part * kPartRows * N;
@@ -534,7 +572,8 @@ __device__ __forceinline__ void tile_product(
                     if (i * 16 < mt.rows && row < mt.rows && col0 < N) {
 #pragma unroll
                         for (int j = 0; j < 2; ++j)
-                            *(f32x4*)(slab + (size_t)row * N + col0 + j * 16 + g16e * 4) = acc[i][j];
+                            if (!FOUR || col0 + j * 16 + g16e * 4 < N)
+                                *(f32x4*)(slab + (size_t)row * N + col0 + j * 16 + g16e * 4) = acc[i][j];
                     }
                 }
             } else {
@@ -576,7 +615,7 @@ __device__ __forceinline__ void tile_product(
                                     v[j][c] = EPI == kEpiRelu ? fmaxf(a, 0.f) : a * sc_of[i];
                                 }
                             store_pair(v[0], v[1], C + (size_t)crow_of[i] * ldc + col0 + g16e * 8,
-                                       (i0 + i) * 16 + l16e < mt.rows && col0 < N);
+                                       (i0 + i) * 16 + l16e < mt.rows && col0 + (FOUR ? g16e * 8 : 0) < N);
                         }
                     }
                 }

@@ -183,7 +183,7 @@ static int layer_step(const moe_layer_step_args* a, bool mx4, void* stream) {
             const moe_ffn_mx4_args f{a->dtype, a->d, a->ffn, E, G * S, 0, G * S, k, a->relu, 0, A, T, a->x, a->assign_of_row,
                                      a->seg_offsets, a->slot_expert, gate, a->packed, a->y_perm, a->workspace_ffn,
                                      a->workspace_ffn_bytes};
-            return mx4_ffn_call(f, st, stage, job);
+            return mx4_ffn_call(f, st, opt, stage, job);
         }
         if (copy_first)
             return grouped_ffn_call(a->relu, a->x_perm, A, nullptr, 1, nullptr, nullptr, a->dtype, A, a->d, a->ffn, E,

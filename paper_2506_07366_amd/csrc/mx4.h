@@ -5,7 +5,7 @@
 //   lane 16 g + c holds columns c (word 2 s) and 16 + c (word 2 s + 1), k = 16 g + 8 s .. + 7 of the k-tile, s = 0, 1.
 // Eight codes are one operand of v_mfma_f32_16x16x32_bf16; the order of k inside an instruction is free as long as both operands
 // have the same, and this one gives a lane 16 neighbours, so that one scale does for its two words and a row's 128 bytes are one cache
-// line for the four lanes that read them.  Four k-tiles (or what is left) are followed by their scales, 256 bytes:
+// line for the four lanes that read them.  Ahead of every four k-tiles (or what is left) are their scales, 256 bytes:
 //   bytes 128 h + 8 c + 2 i + j: k-tile i, column 16 j + c, k = 32 h .. 32 h + 31.
 // In the first product of a SwiGLU FFN a panel is 16 hidden columns: the gate's as columns 0 .. 15, the up projection's as 16 .. 31, so
 // that a lane has both sums of a hidden value.  Padding (k past the end, columns past the end) is zeros.
@@ -24,11 +24,8 @@ __host__ __device__ inline size_t mx4_panel_bytes(int kt) {
     return (size_t)kt * kMx4Block + (size_t)ceil_div(kt, 4) * kMx4Scales;
 }
 // bytes from a panel's start to the codes of k-tile i, and to the scales of its four
-__host__ __device__ inline unsigned mx4_codes_at(int i) { return (unsigned)i * kMx4Block + (unsigned)(i >> 2) * kMx4Scales; }
-__host__ __device__ inline unsigned mx4_scales_at(int i, int kt) {
-    const int end = (i | 3) + 1 < kt ? (i | 3) + 1 : kt;
-    return (unsigned)end * kMx4Block + (unsigned)(i >> 2) * kMx4Scales;
-}
+__host__ __device__ inline unsigned mx4_codes_at(int i) { return (unsigned)i * kMx4Block + (unsigned)((i >> 2) + 1) * kMx4Scales; }
+__host__ __device__ inline unsigned mx4_scales_at(int i) { return (unsigned)(i >> 2) * (4 * kMx4Block + kMx4Scales); }
 
 // One matrix per expert: k-tiles, panels, bytes of an expert.
 struct Mx4Matrix {
@@ -71,6 +68,6 @@ __device__ __forceinline__ float mx4_scale(unsigned bytes) {
 }
 
 // moe_grouped_ffn_mx4, or the part of it that `stage` names (ffn_tables.h).
-int mx4_ffn_call(const moe_ffn_mx4_args& a, hipStream_t st, FfnStage stage, TableJob* job_out);
+int mx4_ffn_call(const moe_ffn_mx4_args& a, hipStream_t st, const FfnOptions& opt, FfnStage stage, TableJob* job_out);
 
 }  // namespace moegps

@@ -6,13 +6,34 @@
 
 namespace moegps {
 
+#include "ffn_tiles.h"
 #include "mx4_stream.h"
+
+// The weights' way into the tiles of ffn_tiles.h: a wavefront's 32 columns are a panel, a k-tile is 16 bytes and two scales per lane.
+struct Mx4Weights {
+    static constexpr bool kFour = true;
+    static __device__ __forceinline__ size_t panel_bytes(int kt) { return mx4_panel_bytes(kt); }
+    static __device__ __forceinline__ unsigned lane_scales(int lane) { return (lane >> 5) * 128 + (lane & 15) * 8; }
+    static __device__ __forceinline__ unsigned codes_at(int i) { return mx4_codes_at(i); }
+    static __device__ __forceinline__ unsigned scales_at(int i) { return mx4_scales_at(i) + (i & 3) * 2; }
+    static __device__ __forceinline__ bf16x8 values(unsigned codes, unsigned scales, int j) {
+        return mx4_values(codes, j ? mx4_scale<1>(scales) : mx4_scale<0>(scales));
+    }
+};
+
+template <int EPI>
+__global__ __launch_bounds__(512, 2) void mx4_tile_kernel(Mx4Product p, int32_t* __restrict__ queues, int n_packed, bool past_caches) {
+    tile_product<EPI, kAlone, Mx4Weights>((const bf16_t*)p.A, p.lda, (const bf16_t*)p.B.at, p.B.expert, (bf16_t*)p.C, p.ldc, p.mtiles,
+                                          p.counts, queues, n_packed, p.B.kt * kMx4K, kTileGroup, past_caches, p.rm, nullptr,
+                                          RowCopy{}, nullptr);
+}
 
 struct Mx4Ws {
     int32_t* rowlist;
-    MTile* tiles;
-    int32_t* counts;
-    void* h;  // hidden activations in row-list order (FFN)
+    MTile* tiles[2];
+    int32_t* counts;  // kCntStride ints per table
+    int32_t* queues;  // per-XCD claim counters of both products
+    void* h;          // hidden activations in row-list order (FFN)
     int capacity;
 };
 
@@ -28,18 +49,33 @@ static size_t mx4_ws_layout(int64_t A, int hidden, int nseg, int dtype, char* ba
     Mx4Ws w;
     w.capacity = (int)(ceil_div64(A1, kMinBM) + nseg);
     w.rowlist = (int32_t*)take((size_t)A1 * sizeof(int32_t));
-    w.tiles = (MTile*)take((size_t)w.capacity * sizeof(MTile));
+    for (int i = 0; i < 2; ++i) w.tiles[i] = (MTile*)take((size_t)w.capacity * sizeof(MTile));
     w.counts = (int32_t*)take(256);
+    w.queues = w.counts ? w.counts + 2 * kCntStride : nullptr;
     w.h = hidden ? take((size_t)A1 * hidden * dtype_size(dtype)) : nullptr;
     if (ws) *ws = w;
     return off;
 }
 
+// Whether a product streams its weights (mx4_stream.h) rather than going by tiles.
+static bool streams(int opt, int dtype, int64_t A, int E) {
+    if (dtype == MOE_DTYPE_F32) return true;
+    if (opt >= 0) return opt > 0;
+    return A <= (int64_t)16 * E;
+}
+
 template <int EPI>
-static int launch_mx4(const Mx4Product& p, int dtype, hipStream_t st) {
-    const bool f32 = dtype == MOE_DTYPE_F32;
-    const auto kern = f32 ? mx4_stream_kernel<1, 8, EPI, true> : mx4_stream_kernel<1, 8, EPI, false>;
-    hipLaunchKernelGGL(kern, dim3(4 * kGemmGrid), dim3(512), 0, st, p);
+static int launch_mx4(const Mx4Product& p, int dtype, bool stream, int E, int32_t* queues, hipStream_t st) {
+    if (stream) {
+        const auto kern = dtype == MOE_DTYPE_F32 ? mx4_stream_kernel<1, 8, EPI, true> : mx4_stream_kernel<1, 8, EPI, false>;
+        hipLaunchKernelGGL(kern, dim3(4 * kGemmGrid), dim3(512), 0, st, p);
+        return check_launch();
+    }
+    const auto kern = mx4_tile_kernel<EPI>;
+    static std::atomic<unsigned long long> raised{0};
+    if (const int rc = raise_lds((const void*)kern, kTileLds<EPI>, raised); rc != MOE_OK) return rc;
+    hipLaunchKernelGGL(kern, dim3(kGemmGrid), dim3(512), kTileLds<EPI>, st, p, queues, EPI == kEpiSwiglu ? 2 * p.N : p.N,
+                       past_caches(E, p.B.expert / sizeof(bf16_t)));
     return check_launch();
 }
 
@@ -62,13 +98,13 @@ static int check_rows(const Mx4Rows& r, int K, int N, int ffn) {
     if (K > kMaxWidth || N > kMaxWidth || ffn > kMaxWidth) return MOE_ERR_UNSUPPORTED;
     if ((size_t)K * dtype_size(r.dtype) % 16 != 0 || (size_t)N * dtype_size(r.dtype) % 16 != 0) return MOE_ERR_UNSUPPORTED;
     const int64_t rows = r.assign_of_row ? r.rows_x : r.A;
-    if (rows >= (1ll << 31) || rows * K >= (1ll << 31)) return MOE_ERR_UNSUPPORTED;
+    if (rows >= (1ll << 31) || rows * K > (1ll << 31) - 64) return MOE_ERR_UNSUPPORTED;  // 32-bit offsets
     if (!r.seg_offsets || !r.slot_expert || !r.packed || !r.workspace) return MOE_ERR_INVALID_ARG;
     if (r.A > 0 && (!r.x || !r.y)) return MOE_ERR_INVALID_ARG;
     return MOE_OK;
 }
 
-int mx4_ffn_call(const moe_ffn_mx4_args& a, hipStream_t st, FfnStage stage, TableJob* job_out) {
+int mx4_ffn_call(const moe_ffn_mx4_args& a, hipStream_t st, const FfnOptions& opt, FfnStage stage, TableJob* job_out) {
     if (a.reserved != 0) return MOE_ERR_INVALID_ARG;
     const Mx4Rows rows{a.dtype, a.E, a.nseg, a.seg_begin, a.seg_end, a.k, a.A, a.rows_x, a.x, a.assign_of_row,
                        a.seg_offsets, a.slot_expert, a.topk_w, a.packed, a.y, a.workspace};
@@ -80,8 +116,14 @@ int mx4_ffn_call(const moe_ffn_mx4_args& a, hipStream_t st, FfnStage stage, Tabl
         if (job_out) *job_out = TableJob{};
         return MOE_OK;
     }
-    const TableSpec t1{ws.tiles, ws.counts, nullptr, kMx4StreamRows, ws.capacity, 0, 0, 1, 0, 0}, none{};
-    const TableJob job{a.E, a.seg_begin, a.seg_end, t1, none, RowLists{ws.rowlist, nullptr, nullptr, 1}, nullptr, 0, nullptr, nullptr};
+    const bool stream = streams(opt.stream, a.dtype, a.A, a.E);
+    // tiles choose their heights by the tiles that a product has, so each has a table of its own
+    const Mx4Matrix m1 = mx4_first(a.packed, a.d, a.ffn, a.relu), m2 = mx4_second(a.packed, a.E, a.d, a.ffn, a.relu);
+    const TableSpec t1{ws.tiles[0], ws.counts, nullptr, stream ? kMx4StreamRows : 0, ws.capacity, m1.kt, 0, ceil_div(m1.panels, 8), 0, 0};
+    const TableSpec t2{stream ? nullptr : ws.tiles[1], ws.counts + kCntStride, nullptr, 0, ws.capacity, m2.kt, 0, ceil_div(m2.panels, 8),
+                       0, 0};
+    const int second = stream ? 0 : 1;
+    const TableJob job{a.E, a.seg_begin, a.seg_end, t1, t2, RowLists{ws.rowlist, nullptr, nullptr, 1}, ws.queues, 16, nullptr, nullptr};
     if (stage == kFfnJobOnly) {
         *job_out = job;
         return MOE_OK;
@@ -90,10 +132,11 @@ int mx4_ffn_call(const moe_ffn_mx4_args& a, hipStream_t st, FfnStage stage, Tabl
         if (const int rc = launch_tables(a.A, a.seg_offsets, a.slot_expert, job, st); rc != MOE_OK) return rc;
     const RowMap rm1{ws.rowlist, a.assign_of_row, a.k, nullptr, nullptr, nullptr};
     const RowMap rm2{nullptr, nullptr, 1, ws.rowlist, a.topk_w ? a.assign_of_row : nullptr, a.topk_w};
-    const Mx4Product p1{a.x, a.d, a.d, mx4_first(a.packed, a.d, a.ffn, a.relu), ws.h, hidden, hidden, ws.tiles, ws.counts, rm1};
-    const Mx4Product p2{ws.h, hidden, hidden, mx4_second(a.packed, a.E, a.d, a.ffn, a.relu), a.y, a.d, a.d, ws.tiles, ws.counts, rm2};
-    const int rc = a.relu ? launch_mx4<kEpiRelu>(p1, a.dtype, st) : launch_mx4<kEpiSwiglu>(p1, a.dtype, st);
-    return rc != MOE_OK ? rc : launch_mx4<kEpiNone>(p2, a.dtype, st);
+    const Mx4Product p1{a.x, a.d, a.d, m1, ws.h, hidden, hidden, ws.tiles[0], ws.counts, rm1};
+    const Mx4Product p2{ws.h, hidden, hidden, m2, a.y, a.d, a.d, ws.tiles[second], ws.counts + second * kCntStride, rm2};
+    const int rc = a.relu ? launch_mx4<kEpiRelu>(p1, a.dtype, stream, a.E, ws.queues, st)
+                          : launch_mx4<kEpiSwiglu>(p1, a.dtype, stream, a.E, ws.queues, st);
+    return rc != MOE_OK ? rc : launch_mx4<kEpiNone>(p2, a.dtype, stream, a.E, ws.queues + 8, st);
 }
 
 }  // namespace moegps
@@ -114,12 +157,15 @@ extern "C" int moe_grouped_product_mx4(const moe_product_mx4_args* a, void* stre
     if (a->workspace_bytes < mx4_ws_layout(a->A, 0, a->nseg, a->dtype, (char*)a->workspace, &ws)) return MOE_ERR_WORKSPACE_TOO_SMALL;
     if (a->A == 0 || a->seg_begin == a->seg_end) return MOE_OK;
     hipStream_t st = (hipStream_t)stream;
-    const TableSpec t1{ws.tiles, ws.counts, nullptr, kMx4StreamRows, ws.capacity, 0, 0, 1, 0, 0}, none{};
-    const TableJob job{a->E, a->seg_begin, a->seg_end, t1, none, RowLists{ws.rowlist, nullptr, nullptr, 1}, nullptr, 0, nullptr, nullptr};
+    const bool streamed = streams(ffn_options().stream, a->dtype, a->A, a->E);
+    const Mx4Matrix m = mx4_matrix(a->packed, a->K, ceil_div(a->N, kMx4N));
+    const TableSpec t1{ws.tiles[0], ws.counts, nullptr, streamed ? kMx4StreamRows : 0, ws.capacity, m.kt, 0, ceil_div(m.panels, 8), 0, 0},
+        none{};
+    const TableJob job{a->E, a->seg_begin, a->seg_end, t1, none, RowLists{ws.rowlist, nullptr, nullptr, 1}, ws.queues, 16, nullptr, nullptr};
     if (const int rc = launch_tables(a->A, a->seg_offsets, a->slot_expert, job, st); rc != MOE_OK) return rc;
     const RowMap rm{ws.rowlist, a->assign_of_row, a->k, ws.rowlist, a->topk_w ? a->assign_of_row : nullptr, a->topk_w};
-    const Mx4Product p{a->x, a->K, a->K, mx4_matrix(a->packed, a->K, ceil_div(a->N, kMx4N)), a->y, a->N, a->N, ws.tiles, ws.counts, rm};
-    return launch_mx4<kEpiNone>(p, a->dtype, st);
+    const Mx4Product p{a->x, a->K, a->K, m, a->y, a->N, a->N, ws.tiles[0], ws.counts, rm};
+    return launch_mx4<kEpiNone>(p, a->dtype, streamed, a->E, ws.queues, st);
 }
 
 extern "C" size_t moe_grouped_ffn_mx4_workspace_bytes(int64_t A, int d, int ffn, int nseg, int dtype) {
@@ -131,5 +177,5 @@ extern "C" size_t moe_grouped_ffn_mx4_workspace_bytes(int64_t A, int d, int ffn,
 extern "C" int moe_grouped_ffn_mx4(const moe_ffn_mx4_args* a, void* stream) {
     using namespace moegps;
     if (!a) return MOE_ERR_INVALID_ARG;
-    return mx4_ffn_call(*a, (hipStream_t)stream, kFfnAll, nullptr);
+    return mx4_ffn_call(*a, (hipStream_t)stream, ffn_options(), kFfnAll, nullptr);
 }

@@ -150,7 +150,7 @@ __global__ __launch_bounds__(256) void mx4_pack_kernel(Mx4Pack p, unsigned char*
         }
         const int panel = threadIdx.x / 32, at = threadIdx.x % 32;  // a panel's 32 pairs of scales
         if (a.p0 + panel < p.panels) {
-            unsigned char* s = to + (a.p0 + panel) * panel_bytes + mx4_scales_at(a.kt, p.kt) + at * 8;
+            unsigned char* s = to + (a.p0 + panel) * panel_bytes + mx4_scales_at(a.kt) + at * 8;
             const unsigned pair = ((const unsigned short*)scales)[panel * 32 + at];
             ((unsigned short*)s)[a.kt & 3] = (unsigned short)pair;
             if (a.kt == p.kt - 1)  // k-tiles that the last four do not have
@@ -182,7 +182,7 @@ __global__ __launch_bounds__(256) void mx4_unpack_kernel(Mx4Pack p, const unsign
             column_of(p, a, c, panel[c], j[c], l16[c]);
             s[c] = 1.f;
             if (a.p0 + panel[c] < p.panels) {
-                const unsigned char* at = from + (a.p0 + panel[c]) * panel_bytes + mx4_scales_at(a.kt, p.kt);
+                const unsigned char* at = from + (a.p0 + panel[c]) * panel_bytes + mx4_scales_at(a.kt);
                 s[c] = __builtin_bit_cast(float, (unsigned)at[a.half * 128 + l16[c] * 8 + (a.kt & 3) * 2 + j[c]] << 23);
             }
         }

@@ -117,7 +117,7 @@ __global__ __launch_bounds__(NW * 64) void mx4_stream_kernel(Mx4Product p) {
 #pragma unroll
                 for (int n = 0; n < NG; ++n) {
                     t.codes[n] = *(const uint4*)(panel[n] + mx4_codes_at(kt) + lane * 16);
-                    t.scales[n] = *(const unsigned short*)(panel[n] + mx4_scales_at(kt, KT) + (g16 >> 1) * 128 + l16 * 8 +
+                    t.scales[n] = *(const unsigned short*)(panel[n] + mx4_scales_at(kt) + (g16 >> 1) * 128 + l16 * 8 +
                                                            (kt & 3) * 2);
                 }
 #pragma unroll

@@ -130,6 +130,14 @@ def test_a_weight_panel_further_than_32_bits():
 # ---------------------------------------------------------------------------
 # products
 # ---------------------------------------------------------------------------
+@pytest.fixture(params=[-1, 0, 1], ids=["auto", "tiles", "streamed"])
+def form(request):
+    """The product's form: by the rule, by tiles, streamed (fp32 rows are streamed in any case)."""
+    B.moe_grouped_ffn_set_option(B.FFN_OPT_STREAM, request.param)
+    yield request.param
+    B.moe_grouped_ffn_set_option(B.FFN_OPT_STREAM, -1)
+
+
 class Batch:
     """Rows of segments: lengths of the segments and the experts that their slots hold (-1: none)."""
 
@@ -186,7 +194,7 @@ RAGGED = [
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("K,N", [(8, 8), (64, 32), (72, 40), (128, 256), (200, 264), (512, 136), (1544, 72)])
 @pytest.mark.parametrize("gather", [False, True])
-def test_product(dtype, K, N, gather):
+def test_product(dtype, K, N, gather, form):
     rng = np.random.default_rng(K + N)
     E = 4
     W = normal(rng, (E, K, N), dtype, 0.05)
@@ -204,7 +212,7 @@ def test_product(dtype, K, N, gather):
 @pytest.mark.parametrize("relu", [False, True])
 @pytest.mark.parametrize("d,ffn", [(8, 1), (64, 64), (136, 65), (72, 200), (512, 100), (256, 1030)])
 @pytest.mark.parametrize("gather", [False, True])
-def test_ffn(dtype, relu, d, ffn, gather):
+def test_ffn(dtype, relu, d, ffn, gather, form):
     rng = np.random.default_rng(d + ffn)
     E = 4
     W1, W3, W2 = (normal(rng, s, dtype, 0.1) for s in ((E, d, ffn), (E, d, ffn), (E, ffn, d)))
@@ -221,7 +229,7 @@ def test_ffn(dtype, relu, d, ffn, gather):
                 dtype, 7.0)
 
 
-def test_slot_ranges():
+def test_slot_ranges(form):
     """A rank's share: rows of the range's segments alone, with the bits that a call over all slots gives them."""
     rng = np.random.default_rng(5)
     E, d, ffn = 4, 128, 96
@@ -244,7 +252,7 @@ def test_slot_ranges():
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("rows", [3, 40, 300])
-def test_infinities_and_nan_stay_where_they_are(dtype, rows):
+def test_infinities_and_nan_stay_where_they_are(dtype, rows, form):
     rng = np.random.default_rng(rows)
     E, K, N = 2, 136, 72
     W = normal(rng, (E, K, N), dtype, 0.1)
@@ -300,7 +308,7 @@ def small_ffn(dtype=BF16, lengths=(30, 0, 75, 11), d=256, ffn=192, seed=3):
 
 
 @pytest.mark.parametrize("lengths", [(1, 0, 1, 0), (30, 0, 75, 11), (700, 0, 301, 5)])
-def test_same_bits_every_time_and_on_another_stream(lengths):
+def test_same_bits_every_time_and_on_another_stream(lengths, form):
     W, b, x, kw = small_ffn(lengths=lengths)
     packed = B.moe_pack_weights_mx4(*W)
     first = B.moe_grouped_ffn_mx4(x, packed=packed, **kw, **b.kwargs())
