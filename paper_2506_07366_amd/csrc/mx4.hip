@@ -21,11 +21,13 @@ struct Mx4Weights {
     }
 };
 
-template <int EPI>
-__global__ __launch_bounds__(512, 2) void mx4_tile_kernel(Mx4Product p, int32_t* __restrict__ queues, int n_packed, bool past_caches) {
-    tile_product<EPI, kAlone, Mx4Weights>((const bf16_t*)p.A, p.lda, (const bf16_t*)p.B.at, p.B.expert, (bf16_t*)p.C, p.ldc, p.mtiles,
-                                          p.counts, queues, n_packed, p.B.kt * kMx4K, kTileGroup, past_caches, p.rm, nullptr,
-                                          RowCopy{}, nullptr);
+// Tiles of up to TALL rows: 256, or 64 by workgroups that run two to a CU.
+template <int EPI, int TALL>
+__global__ __launch_bounds__(512, TALL == kTileMaxRows ? 2 : 4) void mx4_tile_kernel(Mx4Product p, int32_t* __restrict__ queues,
+                                                                                      int n_packed, bool past_caches) {
+    tile_product<EPI, kAlone, Mx4Weights, TALL>((const bf16_t*)p.A, p.lda, (const bf16_t*)p.B.at, p.B.expert, (bf16_t*)p.C, p.ldc,
+                                                p.mtiles, p.counts, queues, n_packed, p.B.kt * kMx4K, kTileGroup, past_caches, p.rm,
+                                                nullptr, RowCopy{}, nullptr);
 }
 
 struct Mx4Ws {
@@ -57,26 +59,47 @@ static size_t mx4_ws_layout(int64_t A, int hidden, int nseg, int dtype, char* ba
     return off;
 }
 
-// Whether a product streams its weights (mx4_stream.h) rather than going by tiles.
-static bool streams(int opt, int dtype, int64_t A, int E) {
-    if (dtype == MOE_DTYPE_F32) return true;
-    if (opt >= 0) return opt > 0;
-    return A <= (int64_t)16 * E;
+// How a product is done: split K, fp32 (mx4_stream.h), tiles of up to 64 or 256 rows (ffn_tiles.h).
+enum Mx4Form { kSplit, kWide, kF32, kShort, kTall };
+constexpr int kFormRows[] = {kMx4SplitRows, kMx4WideRows, kMx4F32Rows, kShortRows, 0};  // of an M-tile; 0: the table builder chooses
+
+// The form goes by the whole batch (A rows, E experts), not by the launched slot range, so that a row gets the same bits from a launch
+// over some slots as from one over all.
+static Mx4Form form_of(int opt, int dtype, int64_t A, int E, const Mx4Matrix& m) {
+    if (dtype == MOE_DTYPE_F32) return kF32;
+    if (opt >= 0) return opt == 0 ? kTall : opt == 1 ? kSplit : kWide;
+    if (A > (int64_t)32 * E) return kTall;
+    return kShort;
 }
 
 template <int EPI>
-static int launch_mx4(const Mx4Product& p, int dtype, bool stream, int E, int32_t* queues, hipStream_t st) {
-    if (stream) {
-        const auto kern = dtype == MOE_DTYPE_F32 ? mx4_stream_kernel<1, 8, EPI, true> : mx4_stream_kernel<1, 8, EPI, false>;
-        hipLaunchKernelGGL(kern, dim3(4 * kGemmGrid), dim3(512), 0, st, p);
+static int launch_mx4(const Mx4Product& p, Mx4Form form, int E, int32_t* queues, hipStream_t st) {
+    auto go = [&](auto kern, int grid, size_t lds, auto... more) {
+        hipLaunchKernelGGL(kern, dim3(grid), dim3(512), lds, st, p, more...);
         return check_launch();
+    };
+    const int n_packed = EPI == kEpiSwiglu ? 2 * p.N : p.N;
+    const bool past = past_caches(E, p.B.expert / sizeof(bf16_t));
+    static std::atomic<unsigned long long> raised{0}, raised_short{0}, raised_wide{0};
+    switch (form) {
+        case kSplit: return go(mx4_split_kernel<EPI>, 4 * kGemmGrid, 0);
+        case kF32: return go(mx4_f32_kernel<EPI>, 4 * kGemmGrid, 0);
+        case kWide: {
+            const auto kern = mx4_wide_kernel<EPI>;
+            if (const int rc = raise_lds((const void*)kern, kMx4WideLds, raised_wide); rc != MOE_OK) return rc;
+            return go(kern, 2 * kGemmGrid, kMx4WideLds);
+        }
+        case kShort: {
+            const auto kern = mx4_tile_kernel<EPI, kShortRows>;
+            if (const int rc = raise_lds((const void*)kern, kShortLds, raised_short); rc != MOE_OK) return rc;
+            return go(kern, 2 * kGemmGrid, kShortLds, queues, n_packed, past);
+        }
+        default: {
+            const auto kern = mx4_tile_kernel<EPI, kTileMaxRows>;
+            if (const int rc = raise_lds((const void*)kern, kStageLds + 16, raised); rc != MOE_OK) return rc;
+            return go(kern, kGemmGrid, kStageLds + 16, queues, n_packed, past);
+        }
     }
-    const auto kern = mx4_tile_kernel<EPI>;
-    static std::atomic<unsigned long long> raised{0};
-    if (const int rc = raise_lds((const void*)kern, kTileLds<EPI>, raised); rc != MOE_OK) return rc;
-    hipLaunchKernelGGL(kern, dim3(kGemmGrid), dim3(512), kTileLds<EPI>, st, p, queues, EPI == kEpiSwiglu ? 2 * p.N : p.N,
-                       past_caches(E, p.B.expert / sizeof(bf16_t)));
-    return check_launch();
 }
 
 // What both calls check; `inner`: the widths whose rows are addressed.
@@ -116,13 +139,15 @@ int mx4_ffn_call(const moe_ffn_mx4_args& a, hipStream_t st, const FfnOptions& op
         if (job_out) *job_out = TableJob{};
         return MOE_OK;
     }
-    const bool stream = streams(opt.stream, a.dtype, a.A, a.E);
-    // tiles choose their heights by the tiles that a product has, so each has a table of its own
     const Mx4Matrix m1 = mx4_first(a.packed, a.d, a.ffn, a.relu), m2 = mx4_second(a.packed, a.E, a.d, a.ffn, a.relu);
-    const TableSpec t1{ws.tiles[0], ws.counts, nullptr, stream ? kMx4StreamRows : 0, ws.capacity, m1.kt, 0, ceil_div(m1.panels, 8), 0, 0};
-    const TableSpec t2{stream ? nullptr : ws.tiles[1], ws.counts + kCntStride, nullptr, 0, ws.capacity, m2.kt, 0, ceil_div(m2.panels, 8),
-                       0, 0};
-    const int second = stream ? 0 : 1;
+    const Mx4Form form1 = form_of(opt.stream, a.dtype, a.A, a.E, m1), form2 = form_of(opt.stream, a.dtype, a.A, a.E, m2);
+    // Products with M-tiles of the same given height share a table; where the builder chooses the height, by the tiles that a product
+    // has, each has its own.
+    const bool own2 = kFormRows[form1] != kFormRows[form2] || form2 == kTall;
+    const TableSpec t1{ws.tiles[0], ws.counts, nullptr, kFormRows[form1], ws.capacity, m1.kt, 0, ceil_div(m1.panels, 8), 0, 0};
+    const TableSpec t2{own2 ? ws.tiles[1] : nullptr, ws.counts + kCntStride, nullptr, kFormRows[form2], ws.capacity, m2.kt, 0,
+                       ceil_div(m2.panels, 8), 0, 0};
+    const int second = own2 ? 1 : 0;
     const TableJob job{a.E, a.seg_begin, a.seg_end, t1, t2, RowLists{ws.rowlist, nullptr, nullptr, 1}, ws.queues, 16, nullptr, nullptr};
     if (stage == kFfnJobOnly) {
         *job_out = job;
@@ -134,9 +159,8 @@ int mx4_ffn_call(const moe_ffn_mx4_args& a, hipStream_t st, const FfnOptions& op
     const RowMap rm2{nullptr, nullptr, 1, ws.rowlist, a.topk_w ? a.assign_of_row : nullptr, a.topk_w};
     const Mx4Product p1{a.x, a.d, a.d, m1, ws.h, hidden, hidden, ws.tiles[0], ws.counts, rm1};
     const Mx4Product p2{ws.h, hidden, hidden, m2, a.y, a.d, a.d, ws.tiles[second], ws.counts + second * kCntStride, rm2};
-    const int rc = a.relu ? launch_mx4<kEpiRelu>(p1, a.dtype, stream, a.E, ws.queues, st)
-                          : launch_mx4<kEpiSwiglu>(p1, a.dtype, stream, a.E, ws.queues, st);
-    return rc != MOE_OK ? rc : launch_mx4<kEpiNone>(p2, a.dtype, stream, a.E, ws.queues + 8, st);
+    const int rc = a.relu ? launch_mx4<kEpiRelu>(p1, form1, a.E, ws.queues, st) : launch_mx4<kEpiSwiglu>(p1, form1, a.E, ws.queues, st);
+    return rc != MOE_OK ? rc : launch_mx4<kEpiNone>(p2, form2, a.E, ws.queues + 8, st);
 }
 
 }  // namespace moegps
@@ -157,15 +181,14 @@ extern "C" int moe_grouped_product_mx4(const moe_product_mx4_args* a, void* stre
     if (a->workspace_bytes < mx4_ws_layout(a->A, 0, a->nseg, a->dtype, (char*)a->workspace, &ws)) return MOE_ERR_WORKSPACE_TOO_SMALL;
     if (a->A == 0 || a->seg_begin == a->seg_end) return MOE_OK;
     hipStream_t st = (hipStream_t)stream;
-    const bool streamed = streams(ffn_options().stream, a->dtype, a->A, a->E);
     const Mx4Matrix m = mx4_matrix(a->packed, a->K, ceil_div(a->N, kMx4N));
-    const TableSpec t1{ws.tiles[0], ws.counts, nullptr, streamed ? kMx4StreamRows : 0, ws.capacity, m.kt, 0, ceil_div(m.panels, 8), 0, 0},
-        none{};
+    const Mx4Form form = form_of(ffn_options().stream, a->dtype, a->A, a->E, m);
+    const TableSpec t1{ws.tiles[0], ws.counts, nullptr, kFormRows[form], ws.capacity, m.kt, 0, ceil_div(m.panels, 8), 0, 0}, none{};
     const TableJob job{a->E, a->seg_begin, a->seg_end, t1, none, RowLists{ws.rowlist, nullptr, nullptr, 1}, ws.queues, 16, nullptr, nullptr};
     if (const int rc = launch_tables(a->A, a->seg_offsets, a->slot_expert, job, st); rc != MOE_OK) return rc;
     const RowMap rm{ws.rowlist, a->assign_of_row, a->k, ws.rowlist, a->topk_w ? a->assign_of_row : nullptr, a->topk_w};
     const Mx4Product p{a->x, a->K, a->K, m, a->y, a->N, a->N, ws.tiles[0], ws.counts, rm};
-    return launch_mx4<kEpiNone>(p, a->dtype, streamed, a->E, ws.queues, st);
+    return launch_mx4<kEpiNone>(p, form, a->E, ws.queues, st);
 }
 
 extern "C" size_t moe_grouped_ffn_mx4_workspace_bytes(int64_t A, int d, int ffn, int nseg, int dtype) {

@@ -130,9 +130,9 @@ def test_a_weight_panel_further_than_32_bits():
 # ---------------------------------------------------------------------------
 # products
 # ---------------------------------------------------------------------------
-@pytest.fixture(params=[-1, 0, 1], ids=["auto", "tiles", "streamed"])
+@pytest.fixture(params=[-1, 0, 1, 2], ids=["auto", "tall", "split", "wide"])
 def form(request):
-    """The product's form: by the rule, by tiles, streamed (fp32 rows are streamed in any case)."""
+    """The form of bf16 products: by the rule, tall tiles, K split between wavefronts, eight panels side by side."""
     B.moe_grouped_ffn_set_option(B.FFN_OPT_STREAM, request.param)
     yield request.param
     B.moe_grouped_ffn_set_option(B.FFN_OPT_STREAM, -1)
@@ -276,6 +276,22 @@ def test_infinities_and_nan_stay_where_they_are(dtype, rows, form):
         ref = host(bad)[[0, rows - 1]] @ Wq[0].numpy()
     got = host(y)[[0, rows - 1]]
     assert np.array_equal(np.isnan(got), np.isnan(ref)) and np.array_equal(got[np.isinf(ref)], ref[np.isinf(ref)])
+
+
+def test_rows_that_end_inside_a_k_tile(form):
+    """What a workgroup has left of other experts' rows, all NaN, is not taken for the end of a row."""
+    rng = np.random.default_rng(4)
+    E, K, N, rows = 16, 72, 10240, 16
+    W = normal(rng, (E, K, N), BF16, 0.1)
+    packed = B.moe_pack_matrix_mx4(W)
+    x = normal(rng, (E * rows, K), BF16)
+    so = torch.arange(0, E * rows + 1, rows, dtype=torch.int32, device="cuda")
+    se = torch.arange(E, dtype=torch.int32, device="cuda")
+    clean = B.moe_grouped_product_mx4(x, so, se, packed, E, N)
+    bad = x.clone().view(E, rows, K)
+    bad[::2] = float("nan")
+    y = B.moe_grouped_product_mx4(bad.view(-1, K), so, se, packed, E, N).view(E, rows, N)
+    assert torch.isnan(y[::2]).all() and torch.equal(y[1::2], clean.view(E, rows, N)[1::2])
 
 
 def test_fp32_rows_of_any_size():
