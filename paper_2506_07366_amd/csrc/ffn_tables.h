@@ -144,12 +144,15 @@ __device__ __forceinline__ int even_height(int rows, int most) {
     return ((rows + n - 1) / n + kHeightStep - 1) / kHeightStep * kHeightStep;
 }
 
-// Row list, and the list of the rows' tokens, rows r being the assignments of[r], `per_token` to a token (null: not wanted).
+// Row list, and the list of the rows' tokens, rows r being the assignments of[r], `per_token` to a token (null: not wanted), and that of
+// their gate weights gate_of[of[r]] (null: not wanted).
 struct RowLists {
     int32_t* rows;
     int32_t* tokens;
     const int32_t* of;
     int per_token;
+    float* gates;
+    const float* gate_of;
 };
 
 // Everything a builder needs to know.
@@ -247,7 +250,11 @@ __device__ __forceinline__ void build_tables(TableScratch<MAXSEG, MAXE, NT>& sh,
             }
             const int r = srt_first[lo] + (p - srt_base[lo]);
             job.lists.rows[p] = r;
-            if (job.lists.tokens) job.lists.tokens[p] = job.lists.of[r] / job.lists.per_token;
+            if (job.lists.tokens) {
+                const int a = job.lists.of[r];
+                job.lists.tokens[p] = a / job.lists.per_token;
+                if (job.lists.gates) job.lists.gates[p] = job.lists.gate_of[a];
+            }
         }
     };
     // tables

@@ -27,8 +27,6 @@ constexpr int kThrough = 16;       // of a buffer store: sc1, written through to
 constexpr int kCacheLine = 128;    // bytes, of the vector L1 and the L2
 constexpr int kCopyPieces = 6;     // pieces of the row copy that a wavefront takes along with a tile
 constexpr size_t kStageLds = (size_t)3 * kTileMaxRows * kPackK * 2;
-constexpr int kShortRows = 64;     // rows of the tallest tile of a launch of short ones: eight stages of them
-constexpr size_t kShortStageLds = (size_t)8 * kShortRows * kPackK * 2, kShortLds = kShortStageLds + 16;
 // dynamic LDS of a workgroup: the stages, in the first product the copy's pieces, the number of the next tile
 template <int EPI>
 constexpr size_t kNextTileAt = kStageLds + (epi_copies(EPI) ? 8 * kCopyPieces * kCopyPieceLds : 0);
@@ -84,9 +82,7 @@ struct PlainWeights {
     static __device__ bf16x8 values(unsigned codes, unsigned scales, int j);
 };
 
-// TALL: rows of the tallest tile of a launch.  With 64 a workgroup takes half of a CU's registers and LDS, two run side by side, and one's
-// prologue and results lie under the other's loads (4-bit weights).
-template <int EPI, int LINK, class Weights = PlainWeights, int TALL = kTileMaxRows>
+template <int EPI, int LINK, class Weights = PlainWeights>
 __device__ __forceinline__ void tile_product(
     const bf16_t* A, int lda,                        // activations [rows, K]
     const bf16_t* __restrict__ Bp, size_t b_stride,  // packed weights [E][N-tile][k-tile][kPackN x kPackK]; in 4 bits
@@ -105,9 +101,9 @@ __device__ __forceinline__ void tile_product(
     constexpr int BN = kPackN, BK = kPackK, NW = 8;
     constexpr int ROW_BYTES = BK * 2;      // of an activation row in a stage
     constexpr int B_BYTES = BN * BK * 2;   // of a weight tile
-    constexpr int TM_MAX = TALL / 16;
+    constexpr int TM_MAX = kTileMaxRows / 16;
     constexpr bool COPIES = epi_copies(EPI) && !FOUR;  // takes a share of the row copy along
-    constexpr size_t kNextAt = !FOUR ? kNextTileAt<EPI> : TALL == kTileMaxRows ? kStageLds : kShortStageLds;
+    constexpr size_t kNextAt = COPIES ? kNextTileAt<EPI> : kStageLds;
 
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
 
@@ -197,10 +193,7 @@ __device__ __forceinline__ void tile_product(
     // start at `run`): no round trip before it, and a workgroup that starts early cannot take it.  In a shared launch
     // workgroups wait for tiles, so only one that runs may own a tile: another launch that waits the same way, on another stream,
     // can keep the rest of this one from starting.  Its counters start at 0.
-    // (So do those that a launch of short tiles has beyond kGemmGrid workgroups.)
-    if (wave == 0)
-        next_tile = LINK == kAlone && (TALL == kTileMaxRows || (int)(blockIdx.x >> 3) < run) ? settle_claim(xcd, (int)(blockIdx.x >> 3))
-                                                                                            : settle_claim(-1, 0);
+    if (wave == 0) next_tile = LINK == kAlone ? settle_claim(xcd, (int)(blockIdx.x >> 3)) : settle_claim(-1, 0);
     int told_expert = -1, told_rows = 0;  // the tile whose results are on their way to memory
     for (;;) {
         lds_wait<0>();                 // thread 0's store of next_tile
@@ -296,14 +289,15 @@ __device__ __forceinline__ void tile_product(
         auto k_loop = [&](auto TM_tag, auto once_tag) {
             constexpr int TM = decltype(TM_tag)::value;
             constexpr int kAux = decltype(once_tag)::value ? kNonTemporal : 0;
-            constexpr int D = Weights::kFour ? (TM <= 4 ? (TALL == kShortRows ? 6 : 8) : TM <= 8 ? 6 : 3) : TM <= 8 ? 4 : 3;  // k-tiles under way
+            // k-tiles under way; 4-bit ones take a quarter of the registers, and are more where the stages have room
+            constexpr int D = FOUR ? (TM <= 4 ? 8 : TM <= 8 ? 6 : 3) : TM <= 8 ? 4 : 3;
             constexpr int STAGE = (FOUR && TM <= 4 ? 64 : TM <= 8 ? 128 : 256) * ROW_BYTES;  // activation bytes of one of them
-            static_assert((size_t)D * STAGE <= (TALL == kTileMaxRows ? kStageLds : kShortStageLds), "LDS of the launch");
+            static_assert((size_t)D * STAGE <= kStageLds, "LDS of the launch");
             constexpr int IA = (TM + 3) / 4;  // activation loads per wavefront and k-tile, 8 rows each
             constexpr int NW_LOADS = FOUR ? 2 : 4;  // of weights
             constexpr int NB = NW_LOADS + IA;       // loads per wavefront and k-tile
             constexpr int NF = 2 * TM;
-            constexpr int R = NF % 8 == 0 && !(FOUR && (TM > 12 || TALL == kShortRows)) ? 8 : 4;
+            constexpr int R = NF % 8 == 0 && !(FOUR && TM > 12) ? 8 : 4;  // (4-bit weights' operands are registers besides: eight spill)
             constexpr int H = NF - R / 2;     // the hand-over opens fragment H
             static_assert(NF % R == 0 && H >= 1, "fragment f sits in register f % R in every k-tile");
             unsigned offA[IA];
@@ -586,16 +580,15 @@ __device__ __forceinline__ void tile_product(
                     }
                 }
             } else {
-                constexpr int RG = TM_MAX < 8 ? TM_MAX : 8;
                 // output row and scale of this lane's rows, fetched eight at a time (one by one each
                 // would wait out a memory round trip, and with it the stores of the row before)
 #pragma unroll
-                for (int i0 = 0; i0 < TM_MAX; i0 += RG) {
+                for (int i0 = 0; i0 < TM_MAX; i0 += 8) {
                     if (i0 * 16 < mt.rows) {
-                        int crow_of[RG];
-                        float sc_of[RG];
+                        int crow_of[8];
+                        float sc_of[8];
 #pragma unroll
-                        for (int i = 0; i < RG; ++i) {
+                        for (int i = 0; i < 8; ++i) {
                             const int row = (i0 + i) * 16 + l16e;
                             crow_of[i] = mt.list0 + (row < mt.rows ? row : mt.rows - 1);
                             sc_of[i] = 1.0f;
@@ -603,18 +596,18 @@ __device__ __forceinline__ void tile_product(
                         if constexpr (EPI == kEpiNone) {
                             if (rm.c_rows) {
 #pragma unroll
-                                for (int i = 0; i < RG; ++i) crow_of[i] = rm.c_rows[crow_of[i]];
+                                for (int i = 0; i < 8; ++i) crow_of[i] = rm.c_rows[crow_of[i]];
                             }
                             if (rm.scale) {
-                                int si[RG];
+                                int si[8];
 #pragma unroll
-                                for (int i = 0; i < RG; ++i) si[i] = rm.scale_idx[crow_of[i]];
+                                for (int i = 0; i < 8; ++i) si[i] = rm.scale_idx[crow_of[i]];
 #pragma unroll
-                                for (int i = 0; i < RG; ++i) sc_of[i] = rm.scale[si[i]];
+                                for (int i = 0; i < 8; ++i) sc_of[i] = rm.scale[si[i]];
                             }
                         }
 #pragma unroll
-                        for (int i = 0; i < RG; ++i) {
+                        for (int i = 0; i < 8; ++i) {
                             if ((i0 + i) * 16 >= mt.rows) continue;
                             float v[2][4];
 #pragma unroll

@@ -21,17 +21,17 @@ struct Mx4Weights {
     }
 };
 
-// Tiles of up to TALL rows: 256, or 64 by workgroups that run two to a CU.
-template <int EPI, int TALL>
-__global__ __launch_bounds__(512, TALL == kTileMaxRows ? 2 : 4) void mx4_tile_kernel(Mx4Product p, int32_t* __restrict__ queues,
-                                                                                      int n_packed, bool past_caches) {
-    tile_product<EPI, kAlone, Mx4Weights, TALL>((const bf16_t*)p.A, p.lda, (const bf16_t*)p.B.at, p.B.expert, (bf16_t*)p.C, p.ldc,
-                                                p.mtiles, p.counts, queues, n_packed, p.B.kt * kMx4K, kTileGroup, past_caches, p.rm,
-                                                nullptr, RowCopy{}, nullptr);
+template <int EPI>
+__global__ __launch_bounds__(512, 2) void mx4_tile_kernel(Mx4Product p, int32_t* __restrict__ queues, int n_packed, bool past_caches) {
+    tile_product<EPI, kAlone, Mx4Weights>((const bf16_t*)p.A, p.lda, (const bf16_t*)p.B.at, p.B.expert, (bf16_t*)p.C, p.ldc, p.mtiles,
+                                          p.counts, queues, n_packed, p.B.kt * kMx4K, kTileGroup, past_caches, p.rm, nullptr,
+                                          RowCopy{}, nullptr);
 }
 
 struct Mx4Ws {
     int32_t* rowlist;
+    int32_t* tokens;  // of the rows at the list's positions, and their gate weights
+    float* gates;
     MTile* tiles[2];
     int32_t* counts;  // kCntStride ints per table
     int32_t* queues;  // per-XCD claim counters of both products
@@ -51,6 +51,8 @@ static size_t mx4_ws_layout(int64_t A, int hidden, int nseg, int dtype, char* ba
     Mx4Ws w;
     w.capacity = (int)(ceil_div64(A1, kMinBM) + nseg);
     w.rowlist = (int32_t*)take((size_t)A1 * sizeof(int32_t));
+    w.tokens = (int32_t*)take((size_t)A1 * sizeof(int32_t));
+    w.gates = (float*)take((size_t)A1 * sizeof(float));
     for (int i = 0; i < 2; ++i) w.tiles[i] = (MTile*)take((size_t)w.capacity * sizeof(MTile));
     w.counts = (int32_t*)take(256);
     w.queues = w.counts ? w.counts + 2 * kCntStride : nullptr;
@@ -59,17 +61,24 @@ static size_t mx4_ws_layout(int64_t A, int hidden, int nseg, int dtype, char* ba
     return off;
 }
 
-// How a product is done: split K, fp32 (mx4_stream.h), tiles of up to 64 or 256 rows (ffn_tiles.h).
-enum Mx4Form { kSplit, kWide, kF32, kShort, kTall };
-constexpr int kFormRows[] = {kMx4SplitRows, kMx4WideRows, kMx4F32Rows, kShortRows, 0};  // of an M-tile; 0: the table builder chooses
+// How a product is done: K split between wavefronts, eight panels side by side, fp32 (mx4_stream.h), tiles of up to 256 rows (ffn_tiles.h).
+enum Mx4Form { kSplit, kWide, kF32, kTiles };
+constexpr int kFormRows[] = {kMx4SplitRows, kMx4WideRows, kMx4F32Rows, 0};  // of an M-tile; 0: the table builder chooses
 
 // The form goes by the whole batch (A rows, E experts), not by the launched slot range, so that a row gets the same bits from a launch
-// over some slots as from one over all.
+// over some slots as from one over all.  Both products, us, split / wide / tiles:
+//   split where eight panels side by side are fewer units than CUs, up to 8 rows per expert: 1 token, top-8 of 128 experts of 4096 x 1536
+//     35 / 38 / 51, top-2 of 8 of 4096 x 14336 51 / 79 / 107, 4 tokens 99 / 115 / 162, 16 tokens (the second product alone) 126 / 140 / 181;
+//   wide up to 24 rows per expert: 128 tokens, top-8 of 128 312 / 204 / 223, 64, top-2 of 8 232 / 179 / 216, 200, top-6 of 64 of 2048 x 1408
+//     147 / 79 / 88, but 512, top-8 of 128 - / 332 / 320, 777, top-6 of 64 - / 162 / 139; up to 128 where tiles would not
+//     go once round the chip: 400, top-4 of 16 of 4096 x 688, first product alone 46 / 30 / 40.
 static Mx4Form form_of(int opt, int dtype, int64_t A, int E, const Mx4Matrix& m) {
     if (dtype == MOE_DTYPE_F32) return kF32;
-    if (opt >= 0) return opt == 0 ? kTall : opt == 1 ? kSplit : kWide;
-    if (A > (int64_t)32 * E) return kTall;
-    return kShort;
+    if (opt >= 0) return opt == 0 ? kTiles : opt == 1 ? kSplit : kWide;
+    const int64_t experts = A < E ? A : E, across = ceil_div(m.panels, 8);
+    if (A <= (int64_t)8 * E && experts * across < kGemmGrid) return kSplit;
+    if (A <= (int64_t)24 * E) return kWide;
+    return A <= (int64_t)128 * E && (ceil_div64(A, 128) + E) * across < kGemmGrid ? kWide : kTiles;
 }
 
 template <int EPI>
@@ -80,7 +89,7 @@ static int launch_mx4(const Mx4Product& p, Mx4Form form, int E, int32_t* queues,
     };
     const int n_packed = EPI == kEpiSwiglu ? 2 * p.N : p.N;
     const bool past = past_caches(E, p.B.expert / sizeof(bf16_t));
-    static std::atomic<unsigned long long> raised{0}, raised_short{0}, raised_wide{0};
+    static std::atomic<unsigned long long> raised{0}, raised_wide{0};
     switch (form) {
         case kSplit: return go(mx4_split_kernel<EPI>, 4 * kGemmGrid, 0);
         case kF32: return go(mx4_f32_kernel<EPI>, 4 * kGemmGrid, 0);
@@ -89,13 +98,8 @@ static int launch_mx4(const Mx4Product& p, Mx4Form form, int E, int32_t* queues,
             if (const int rc = raise_lds((const void*)kern, kMx4WideLds, raised_wide); rc != MOE_OK) return rc;
             return go(kern, 2 * kGemmGrid, kMx4WideLds);
         }
-        case kShort: {
-            const auto kern = mx4_tile_kernel<EPI, kShortRows>;
-            if (const int rc = raise_lds((const void*)kern, kShortLds, raised_short); rc != MOE_OK) return rc;
-            return go(kern, 2 * kGemmGrid, kShortLds, queues, n_packed, past);
-        }
         default: {
-            const auto kern = mx4_tile_kernel<EPI, kTileMaxRows>;
+            const auto kern = mx4_tile_kernel<EPI>;
             if (const int rc = raise_lds((const void*)kern, kStageLds + 16, raised); rc != MOE_OK) return rc;
             return go(kern, kGemmGrid, kStageLds + 16, queues, n_packed, past);
         }
@@ -127,6 +131,11 @@ static int check_rows(const Mx4Rows& r, int K, int N, int ffn) {
     return MOE_OK;
 }
 
+// The lists that the table builder makes: with rows that are gathered their tokens (looked up once, not twice for every tile), and their gate weights.
+static RowLists row_lists(const Mx4Rows& r, const Mx4Ws& ws) {
+    return RowLists{ws.rowlist, r.assign_of_row ? ws.tokens : nullptr, r.assign_of_row, r.k, r.topk_w ? ws.gates : nullptr, r.topk_w};
+}
+
 int mx4_ffn_call(const moe_ffn_mx4_args& a, hipStream_t st, const FfnOptions& opt, FfnStage stage, TableJob* job_out) {
     if (a.reserved != 0) return MOE_ERR_INVALID_ARG;
     const Mx4Rows rows{a.dtype, a.E, a.nseg, a.seg_begin, a.seg_end, a.k, a.A, a.rows_x, a.x, a.assign_of_row,
@@ -143,22 +152,23 @@ int mx4_ffn_call(const moe_ffn_mx4_args& a, hipStream_t st, const FfnOptions& op
     const Mx4Form form1 = form_of(opt.stream, a.dtype, a.A, a.E, m1), form2 = form_of(opt.stream, a.dtype, a.A, a.E, m2);
     // Products with M-tiles of the same given height share a table; where the builder chooses the height, by the tiles that a product
     // has, each has its own.
-    const bool own2 = kFormRows[form1] != kFormRows[form2] || form2 == kTall;
+    const bool own2 = kFormRows[form1] != kFormRows[form2] || form2 == kTiles;
     const TableSpec t1{ws.tiles[0], ws.counts, nullptr, kFormRows[form1], ws.capacity, m1.kt, 0, ceil_div(m1.panels, 8), 0, 0};
     const TableSpec t2{own2 ? ws.tiles[1] : nullptr, ws.counts + kCntStride, nullptr, kFormRows[form2], ws.capacity, m2.kt, 0,
                        ceil_div(m2.panels, 8), 0, 0};
     const int second = own2 ? 1 : 0;
-    const TableJob job{a.E, a.seg_begin, a.seg_end, t1, t2, RowLists{ws.rowlist, nullptr, nullptr, 1}, ws.queues, 16, nullptr, nullptr};
+    const TableJob job{a.E, a.seg_begin, a.seg_end, t1, t2, row_lists(rows, ws), ws.queues, 16, nullptr, nullptr};
     if (stage == kFfnJobOnly) {
         *job_out = job;
         return MOE_OK;
     }
     if (stage == kFfnAll)
         if (const int rc = launch_tables(a.A, a.seg_offsets, a.slot_expert, job, st); rc != MOE_OK) return rc;
-    const RowMap rm1{ws.rowlist, a.assign_of_row, a.k, nullptr, nullptr, nullptr};
+    const RowMap rm1{a.assign_of_row ? ws.tokens : ws.rowlist, nullptr, 1, nullptr, nullptr, nullptr};
     const RowMap rm2{nullptr, nullptr, 1, ws.rowlist, a.topk_w ? a.assign_of_row : nullptr, a.topk_w};
-    const Mx4Product p1{a.x, a.d, a.d, m1, ws.h, hidden, hidden, ws.tiles[0], ws.counts, rm1};
-    const Mx4Product p2{ws.h, hidden, hidden, m2, a.y, a.d, a.d, ws.tiles[second], ws.counts + second * kCntStride, rm2};
+    const Mx4Product p1{a.x, a.d, a.d, m1, ws.h, hidden, hidden, ws.tiles[0], ws.counts, rm1, nullptr};
+    const Mx4Product p2{ws.h, hidden, hidden, m2, a.y, a.d, a.d, ws.tiles[second], ws.counts + second * kCntStride, rm2,
+                        a.topk_w ? ws.gates : nullptr};
     const int rc = a.relu ? launch_mx4<kEpiRelu>(p1, form1, a.E, ws.queues, st) : launch_mx4<kEpiSwiglu>(p1, form1, a.E, ws.queues, st);
     return rc != MOE_OK ? rc : launch_mx4<kEpiNone>(p2, form2, a.E, ws.queues + 8, st);
 }
@@ -184,10 +194,11 @@ extern "C" int moe_grouped_product_mx4(const moe_product_mx4_args* a, void* stre
     const Mx4Matrix m = mx4_matrix(a->packed, a->K, ceil_div(a->N, kMx4N));
     const Mx4Form form = form_of(ffn_options().stream, a->dtype, a->A, a->E, m);
     const TableSpec t1{ws.tiles[0], ws.counts, nullptr, kFormRows[form], ws.capacity, m.kt, 0, ceil_div(m.panels, 8), 0, 0}, none{};
-    const TableJob job{a->E, a->seg_begin, a->seg_end, t1, none, RowLists{ws.rowlist, nullptr, nullptr, 1}, ws.queues, 16, nullptr, nullptr};
+    const TableJob job{a->E, a->seg_begin, a->seg_end, t1, none, row_lists(rows, ws), ws.queues, 16, nullptr, nullptr};
     if (const int rc = launch_tables(a->A, a->seg_offsets, a->slot_expert, job, st); rc != MOE_OK) return rc;
-    const RowMap rm{ws.rowlist, a->assign_of_row, a->k, ws.rowlist, a->topk_w ? a->assign_of_row : nullptr, a->topk_w};
-    const Mx4Product p{a->x, a->K, a->K, m, a->y, a->N, a->N, ws.tiles[0], ws.counts, rm};
+    const RowMap rm{a->assign_of_row ? ws.tokens : ws.rowlist, nullptr, 1, ws.rowlist, a->topk_w ? a->assign_of_row : nullptr, a->topk_w};
+    const Mx4Product p{a->x, a->K, a->K, m, a->y, a->N, a->N, ws.tiles[0], ws.counts, rm,
+                       a->topk_w ? ws.gates : nullptr};
     return launch_mx4<kEpiNone>(p, form, a->E, ws.queues, st);
 }
 

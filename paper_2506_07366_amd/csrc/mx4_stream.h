@@ -46,7 +46,8 @@ struct Mx4Product {
     int ldc, N;
     const MTile* mtiles;
     const int32_t* counts;
-    RowMap rm;
+    RowMap rm;           // (without rows to look up twice)
+    const float* gates;  // of the rows, by list position; null: none
 };
 
 constexpr int kMx4SplitWaves = 8;
@@ -87,8 +88,8 @@ __device__ __forceinline__ void add_parts(const Mx4Product& p, float* xch, int w
         int crow = list0 + row;
         float sc = 1.f;
         if (EPI == kEpiNone) {
+            if (p.gates) sc = p.gates[crow];
             if (p.rm.c_rows) crow = p.rm.c_rows[crow];
-            if (p.rm.scale) sc = p.rm.scale[p.rm.scale_idx[crow]];
         }
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
@@ -114,15 +115,8 @@ constexpr unsigned kRowRange = 0xffffff80u, kRowPast = 0xfffffff0u;  // of the r
 __device__ __forceinline__ auto rows_rsrc(const Mx4Product& p) {
     return __builtin_amdgcn_make_buffer_rsrc((void*)p.A, 0, (int)kRowRange, 0x00027000);
 }
-// byte offset of a row of the product's operand
-__device__ __forceinline__ unsigned row_offset(const Mx4Product& p, int pos) {
-    int r = pos;
-    if (p.rm.a_rows) {
-        r = p.rm.a_rows[r];
-        if (p.rm.a_rows2) r = p.rm.a_rows2[r] / p.rm.a_div;
-    }
-    return (unsigned)r * (unsigned)p.lda * 2u;
-}
+// row of the product's operand at a list position
+__device__ __forceinline__ int row_at(const Mx4Product& p, int pos) { return p.rm.a_rows ? p.rm.a_rows[pos] : pos; }
 template <int AUX, class R>
 __device__ __forceinline__ void load_step(Mx4Step& t, R rsrc, int step, bool in, int lane) {
     const unsigned at = in ? (unsigned)step * kStepBytes : 0xf0000000u;
@@ -178,7 +172,7 @@ __global__ __launch_bounds__(kMx4SplitWaves * 64, 4) void mx4_split_kernel(Mx4Pr
                 const int row = i * 8 + (lane >> 3), slot = (lane & 7) ^ swz(row);
                 a_end[i] = ((p.K >> 3) - slot + 7) / 8;
                 const int at = row0 + row < mt.rows ? row0 + row : mt.rows - 1;  // rows past the end repeat the last one
-                off[i] = row_offset(p, mt.list0 + at) + slot * 16u;
+                off[i] = (unsigned)row_at(p, mt.list0 + at) * (unsigned)p.lda * 2u + slot * 16u;
             }
             unsigned a_lane[2];
 #pragma unroll
@@ -293,7 +287,7 @@ __global__ __launch_bounds__(512, 4) void mx4_wide_kernel(Mx4Product p) {
                 const int piece = wave + i * NW, row = (piece % (2 * TM)) * 8 + (lane >> 3), at = (lane & 7) ^ swz(row);
                 a_kt[i] = piece / (2 * TM);
                 a_end[i] = ((p.K >> 3) - at + 7) / 8;
-                off[i] = row_offset(p, mt.list0 + (row < mt.rows ? row : mt.rows - 1)) + at * 16u;
+                off[i] = (unsigned)row_at(p, mt.list0 + (row < mt.rows ? row : mt.rows - 1)) * (unsigned)p.lda * 2u + at * 16u;
             }
             f32x4 acc[TM][2];
 #pragma unroll
@@ -362,8 +356,8 @@ __global__ __launch_bounds__(512, 4) void mx4_wide_kernel(Mx4Product p) {
                 int crow = mt.list0 + row;
                 float sc = 1.f;
                 if (EPI == kEpiNone) {
+                    if (p.gates) sc = p.gates[crow];
                     if (p.rm.c_rows) crow = p.rm.c_rows[crow];
-                    if (p.rm.scale) sc = p.rm.scale[p.rm.scale_idx[crow]];
                 }
                 bf16_t* out = (bf16_t*)p.C + (size_t)crow * p.ldc + col0;
 #pragma unroll
@@ -414,11 +408,7 @@ __global__ __launch_bounds__(kMx4SplitWaves * 64) void mx4_f32_kernel(Mx4Product
 #pragma unroll
             for (int i = 0; i < MT; ++i) {
                 int r = i * 16 + l16;
-                r = mt.list0 + (r < mt.rows ? r : mt.rows - 1);
-                if (p.rm.a_rows) {
-                    r = p.rm.a_rows[r];
-                    if (p.rm.a_rows2) r = p.rm.a_rows2[r] / p.rm.a_div;
-                }
+                r = row_at(p, mt.list0 + (r < mt.rows ? r : mt.rows - 1));
                 arow[i] = (const char*)p.A + (size_t)r * p.lda * 4;
             }
             f32x4 acc[MT][NG][2];
