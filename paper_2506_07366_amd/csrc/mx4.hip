@@ -1,7 +1,9 @@
 // Grouped products and the experts' FFN with weights in 4 bits (include/moegps_mx4.h; layout: mx4.h).
 //
 // Rows are tiled by expert, as in grouped_ffn.hip: the rows of all segments of an expert are listed one after the other by the table
-// builder (ffn_tables.h) and cut into M-tiles together.
+// builder (ffn_tables.h) and cut into M-tiles together.  Bound by the weights' bytes up to some 50 rows per expert, then by the matrix
+// pipe.  Both products, us, bf16 weights -> 4 bits: 128 tokens, top-8 of 128 experts of 4096 x 1536 503 -> 200, 16, top-2 of 8 of 4096 x
+// 14336 280 -> 121, 4096 2264 -> 2052 (1.41 PFLOP/s).
 #include "mx4.h"
 
 namespace moegps {
@@ -72,8 +74,11 @@ constexpr int kFormRows[] = {kMx4SplitRows, kMx4WideRows, kMx4F32Rows, 0};  // o
 //   wide up to 24 rows per expert: 128 tokens, top-8 of 128 312 / 204 / 223, 64, top-2 of 8 232 / 179 / 216, 200, top-6 of 64 of 2048 x 1408
 //     147 / 79 / 88, but 512, top-8 of 128 - / 332 / 320, 777, top-6 of 64 - / 162 / 139; up to 128 where tiles would not
 //     go once round the chip: 400, top-4 of 16 of 4096 x 688, first product alone 46 / 30 / 40.
-static Mx4Form form_of(int opt, int dtype, int64_t A, int E, const Mx4Matrix& m) {
+// Hidden rows of 2^31 values and more are left to the tiles, which address them from the tile's first row; the others have 32-bit
+// offsets into all of them.  values: of the product's rows.
+static Mx4Form form_of(int opt, int dtype, int64_t A, int E, const Mx4Matrix& m, int64_t values) {
     if (dtype == MOE_DTYPE_F32) return kF32;
+    if (values > (1ll << 31) - 64) return kTiles;
     if (opt >= 0) return opt == 0 ? kTiles : opt == 1 ? kSplit : kWide;
     const int64_t experts = A < E ? A : E, across = ceil_div(m.panels, 8);
     if (A <= (int64_t)8 * E && experts * across < kGemmGrid) return kSplit;
@@ -106,7 +111,7 @@ static int launch_mx4(const Mx4Product& p, Mx4Form form, int E, int32_t* queues,
     }
 }
 
-// What both calls check; `inner`: the widths whose rows are addressed.
+// What both calls check.
 struct Mx4Rows {
     int dtype, E, nseg, seg_begin, seg_end, k;
     int64_t A, rows_x;
@@ -149,7 +154,7 @@ int mx4_ffn_call(const moe_ffn_mx4_args& a, hipStream_t st, const FfnOptions& op
         return MOE_OK;
     }
     const Mx4Matrix m1 = mx4_first(a.packed, a.d, a.ffn, a.relu), m2 = mx4_second(a.packed, a.E, a.d, a.ffn, a.relu);
-    const Mx4Form form1 = form_of(opt.stream, a.dtype, a.A, a.E, m1), form2 = form_of(opt.stream, a.dtype, a.A, a.E, m2);
+    const Mx4Form form1 = form_of(opt.stream, a.dtype, a.A, a.E, m1, 0), form2 = form_of(opt.stream, a.dtype, a.A, a.E, m2, a.A * hidden);
     // Products with M-tiles of the same given height share a table; where the builder chooses the height, by the tiles that a product
     // has, each has its own.
     const bool own2 = kFormRows[form1] != kFormRows[form2] || form2 == kTiles;
@@ -192,7 +197,7 @@ extern "C" int moe_grouped_product_mx4(const moe_product_mx4_args* a, void* stre
     if (a->A == 0 || a->seg_begin == a->seg_end) return MOE_OK;
     hipStream_t st = (hipStream_t)stream;
     const Mx4Matrix m = mx4_matrix(a->packed, a->K, ceil_div(a->N, kMx4N));
-    const Mx4Form form = form_of(ffn_options().stream, a->dtype, a->A, a->E, m);
+    const Mx4Form form = form_of(ffn_options().stream, a->dtype, a->A, a->E, m, 0);
     const TableSpec t1{ws.tiles[0], ws.counts, nullptr, kFormRows[form], ws.capacity, m.kt, 0, ceil_div(m.panels, 8), 0, 0}, none{};
     const TableJob job{a->E, a->seg_begin, a->seg_end, t1, none, row_lists(rows, ws), ws.queues, 16, nullptr, nullptr};
     if (const int rc = launch_tables(a->A, a->seg_offsets, a->slot_expert, job, st); rc != MOE_OK) return rc;

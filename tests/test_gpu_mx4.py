@@ -278,6 +278,23 @@ def test_infinities_and_nan_stay_where_they_are(dtype, rows, form):
     assert np.array_equal(np.isnan(got), np.isnan(ref)) and np.array_equal(got[np.isinf(ref)], ref[np.isinf(ref)])
 
 
+def test_hidden_rows_past_32_bits(form):
+    """Hidden activations of more than 2^32 bytes: what their last rows make."""
+    rng = np.random.default_rng(6)
+    E, d, ffn, A = 2, 64, 65600, 33000
+    assert A * ffn * 2 > 2 ** 32
+    W = [normal(rng, s, BF16, 0.1) for s in ((E, d, ffn), (E, d, ffn), (E, ffn, d))]
+    packed = B.moe_pack_weights_mx4(*W)
+    x = normal(rng, (A, d), BF16)
+    so = torch.tensor([0, 200, A], dtype=torch.int32, device="cuda")
+    se = torch.tensor([0, 1], dtype=torch.int32, device="cuda")
+    y = B.moe_grouped_ffn_mx4(x, so, se, packed, E, ffn)
+    for e, rows in ((0, slice(0, 3)), (1, slice(A - 5, A))):
+        Q = [mx.quantise(host(w[e])) for w in W]
+        ref, tol = mx.ffn(host(x[rows]), *Q, U_SUM, u_of(BF16))
+        assert (np.abs(host(y[rows]) - ref) <= tol + u_of(BF16) * (np.abs(ref) + tol)).all()
+
+
 def test_rows_that_end_inside_a_k_tile(form):
     """What a workgroup has left of other experts' rows, all NaN, is not taken for the end of a row."""
     rng = np.random.default_rng(4)
