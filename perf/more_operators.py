@@ -157,10 +157,18 @@ def _kept(gen, experts, k, n, dtype):
 
 
 def _dense(kept, dtype):
+    """Values of codes and scales in dtype, where they are exact: what a program that holds a 4-bit checkpoint makes of it, once, for
+    moe_pack_weights_mx4.  Two codes are one look-up; a scale's byte is the exponent field of its power of two."""
     codes, scales = kept
-    w = torch.empty(codes.shape, dtype=dtype, device="cuda")
-    for e in range(codes.shape[0]):
-        w[e] = _from_codes(codes[e], scales[e]).to(dtype)
+    whole = codes.shape[1] // GROUP
+    table = torch.tensor(VALUES + tuple(-v for v in VALUES), device="cuda", dtype=dtype)
+    pair = torch.arange(16 * 256, device="cuda")
+    pairs = table[torch.stack((pair % 16, pair // 256), dim=1)]
+    two = torch.int32 if dtype == torch.bfloat16 else torch.int64
+    w = pairs.view(two).view(-1).index_select(0, codes.view(-1).view(torch.int16).int()).view(dtype).view(codes.shape)
+    scale = (scales.short() << 7).view(dtype) if dtype == torch.bfloat16 else (scales.int() << 23).view(dtype)
+    w[:, :whole * GROUP].unflatten(1, (whole, GROUP)).mul_(scale[:, :whole].unsqueeze(2))
+    w[:, whole * GROUP:].mul_(scale[:, whole:])
     return w
 
 
