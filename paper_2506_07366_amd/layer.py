@@ -78,6 +78,7 @@ class MoELayer:
     def set_weights(self, W1: torch.Tensor, W3: Optional[torch.Tensor], W2: torch.Tensor) -> None:
         """One-off repack of the (static) expert weights, into a new buffer; the ReLU form has no W3.  In training, where
         they change, they are laid out for both passes and in the same buffers every time: a recorded graph reads those set last."""
+        self._need_weights(W1, W3, W2)
         if self.mx4:
             self.packed = B.moe_pack_weights_mx4(W1, None if self.cfg.act == "relu" else W3, W2)
             return
@@ -94,6 +95,16 @@ class MoELayer:
             self.packed_backward = B.moe_pack_weights_backward(W1, None if self.cfg.act == "relu" else W3, W2,
                                                                out=place_backward)
             self._packed_places = self.packed, self.packed_backward
+
+    def _need_weights(self, W1, W3, W2) -> None:
+        """Weights of this layer's shapes: once packed they are bytes, and other shapes (transposed ones, say) have as many."""
+        c = self.cfg
+        B._need_shape(W1, (c.E, c.d, c.ffn), "W1")
+        B._need_shape(W2, (c.E, c.ffn, c.d), "W2")
+        if c.act != "relu":
+            if W3 is None:
+                raise B.MoeGpsError("SwiGLU experts have a W3")
+            B._need_shape(W3, (c.E, c.d, c.ffn), "W3")
 
     # individual steps (each is exactly one C-ABI call) ---------------------
     def route(self, logits):
