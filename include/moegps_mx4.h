@@ -20,9 +20,11 @@ extern "C" {
  *     b      the smallest with max|w| <= 6 * 2^(b - 127), between 2 and 253; 127 for a group of zeros
  *     codes  e2m1: a sign and one of 0, 0.5, 1, 1.5, 2, 3, 4, 6; w / 2^(b - 127) to the nearest, ties to the one whose last bit is 0.
  *            What would be rounded to 2^128 is held as 3 * 2^126: finite weights stay finite
- * A weight is off by a fifth of itself at most (2.5 held as 2) while it is 2^(b - 127) or more, and by 2^(b - 129) below.  What is held,
- * code * 2^(b - 127), is exact in bf16 and in fp32, so packing what moe_unpack_weights_mx4 gives back holds the same values: weights that come
- * in this format from elsewhere are packed from their values without loss.  A group that holds an infinity or a NaN is all NaN.
+ * A weight below 3.5 * 2^126 is off by a fifth of itself at most (2.5 held as 2) while it is 2^(b - 127) or more, and by 2^(b - 129) below;
+ * one from there up, being held as 3 * 2^126, by a quarter.  What is held, code * 2^(b - 127), is exact in bf16 and in fp32, so packing what
+ * moe_unpack_weights_mx4 gives back holds the same values.  Weights that come in such a format from elsewhere are packed from their values
+ * without loss where their scales' bytes are 2 to 253 and none is above 3 * 2^126 (bytes of 0 and 1 have values that are no multiples of
+ * 2^-126, which are rounded).  A group that holds an infinity or a NaN is all NaN.
  *
  * moe_pack_weights_mx4 brings the weights of an FFN to 4 bits and lays them out for moe_grouped_ffn_mx4:
  *   W1, W3 [E, d, ffn], W2 [E, ffn, d]  dtype in (row-major); W3 NULL: the ReLU form, without a gate matrix
@@ -30,7 +32,8 @@ extern "C" {
  * moe_unpack_weights_mx4 gives the values back, in dtype: the gradient through experts that stay as they are is
  * moe_grouped_ffn_backward with these values packed for it.  An output may be NULL, not wanted (W3 is with relu).
  * moe_pack_matrix_mx4 and moe_unpack_matrix_mx4 do the same with one matrix per expert, W [E, K, N], for moe_grouped_product_mx4.
- * The layout is opaque and the same whatever is packed into it.
+ * The layout is opaque and the same whatever is packed into it: it does not say which widths or which form it was packed for, and is read
+ * with those that it was packed with (other widths may have as many bytes).
  * Limits: 1 <= E <= MOE_MAX_EXPERTS, widths up to 2^22, any of them.  Size queries return 0 outside.
  */
 #define MOE_MX4_GROUP 32
