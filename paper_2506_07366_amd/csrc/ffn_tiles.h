@@ -565,7 +565,8 @@ __device__ __forceinline__ void tile_product(
         } else {
             const int col0 = n0 + wave * 32;  // (plain weights: N is a multiple of 64, the wavefront's columns exist or not together)
             float* slab = nullptr;
-            if constexpr (EPI == kEpiNone && LINK == kAlone)
+            static_assert(!FOUR || EPI != kEpiFloat, "4-bit weights: sums are rounded to the rows' type");
+            if constexpr (EPI == kEpiNone && LINK == kAlone && !FOUR)  // (their tables have no parts)
                 if (mt.part >= 0) slab = partials + (size_t)mt.part * kPartRows * N;
             if constexpr (EPI == kEpiFloat) slab = partials + (size_t)mt.list0 * N;
             if (EPI == kEpiFloat || slab) {
@@ -575,8 +576,7 @@ __device__ __forceinline__ void tile_product(
                     if (i * 16 < mt.rows && row < mt.rows && col0 < N) {
 #pragma unroll
                         for (int j = 0; j < 2; ++j)
-                            if (!FOUR || col0 + j * 16 + g16e * 4 < N)
-                                *(f32x4*)(slab + (size_t)row * N + col0 + j * 16 + g16e * 4) = acc[i][j];
+                            *(f32x4*)(slab + (size_t)row * N + col0 + j * 16 + g16e * 4) = acc[i][j];
                     }
                 }
             } else {

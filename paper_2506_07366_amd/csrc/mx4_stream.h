@@ -1,10 +1,13 @@
-// Products with 4-bit weights whose wavefronts split K between them.  Included by mx4.hip inside namespace moegps.
+// Products with 4-bit weights that go along the panels' bytes.  Included by mx4.hip inside namespace moegps.
 //
-// A unit is an M-tile by NG panels (32 packed columns each).  The eight wavefronts of a workgroup share the unit's columns, and nothing
-// synchronises until the fp32 sums are added up through LDS, wavefront 0 first, so the result does not depend on timing.
-//   mx4_split_kernel  bf16 rows, up to 32 of them: the finest units, for batches whose tiles would not fill the chip
+//   mx4_split_kernel  bf16 rows, M-tiles of up to 32: the finest units, for batches whose tiles would not fill the chip
+//   mx4_wide_kernel   bf16 rows, M-tiles of up to 32: eight panels side by side, for many units of few rows
 //   mx4_f32_kernel    fp32 rows, any number: x = hi + mid + lo by cutting off 8 significant bits at a time, exact, and so are
 //                     the products with the weights, which are exact in bf16
+//
+// In the first and the last a unit is an M-tile by one panel.  The eight wavefronts of a workgroup split K between them, and nothing
+// synchronises until their fp32 sums are added up through LDS, wavefront 0 first, so the result does not depend on timing.  In the wide
+// form a wavefront has a panel and all of K to itself, the rows are everybody's, and there is a barrier for every step of 256 of K.
 #pragma once
 
 typedef __attribute__((__vector_size__(2 * sizeof(unsigned)))) unsigned u32x2;
@@ -55,35 +58,30 @@ constexpr int kMx4SplitRows = 32, kMx4F32Rows = 64;  // rows of an M-tile
 
 // Adds up what the wavefronts have of rows list0 + row0 .. of an M-tile with `rows` from there on (16 at most are there) and stores
 // the results.  Starts and ends with a barrier's worth of order: xch may be anything that all wavefronts are done with.
-template <int NG, int EPI, bool F32>
-__device__ __forceinline__ void add_parts(const Mx4Product& p, float* xch, int wave, const f32x4 (&acc)[NG][2], int list0, int rows,
-                                          int unit) {
+template <int EPI, bool F32>
+__device__ __forceinline__ void add_parts(const Mx4Product& p, float* xch, int wave, const f32x4 (&acc)[2], int list0, int rows,
+                                          int panel) {
     constexpr bool SWIGLU = EPI == kEpiSwiglu;
-    constexpr int UC = NG * kMx4N;              // packed columns of a unit
-    constexpr int OC = SWIGLU ? UC / 2 : UC;    // output columns
-    constexpr int PITCH = UC + 4;
+    constexpr int OC = SWIGLU ? kMx4N / 2 : kMx4N;  // output columns
+    constexpr int PITCH = kMx4N + 4;
     const int lane = threadIdx.x & 63, l16 = lane & 15, g16 = lane >> 4;
     __syncthreads();
     if (l16 < rows)
 #pragma unroll
-        for (int n = 0; n < NG; ++n)
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-                *(f32x4*)&xch[(wave * 16 + l16) * PITCH + n * kMx4N + j * 16 + g16 * 4] = acc[n][j];
+        for (int j = 0; j < 2; ++j) *(f32x4*)&xch[(wave * 16 + l16) * PITCH + j * 16 + g16 * 4] = acc[j];
     __syncthreads();
     for (int at = threadIdx.x; at < 16 * OC / 2; at += kMx4SplitWaves * 64) {
         const int row = at / (OC / 2), c = at % (OC / 2) * 2;
-        // packed column of the first: with SwiGLU 16 gate columns and their 16 up columns alternate
-        const int pc = SWIGLU ? (c >> 4) * kMx4N + (c & 15) : c;
-        const int col = unit * OC + c;
+        // (with SwiGLU the panel's first 16 columns are the gate's, their up columns the others)
+        const int col = panel * OC + c;
         if (row >= rows || col >= p.N) continue;
         float v[2] = {0.f, 0.f}, g[2] = {0.f, 0.f};
 #pragma unroll
         for (int w = 0; w < kMx4SplitWaves; ++w)
 #pragma unroll
             for (int q = 0; q < 2; ++q) {
-                v[q] += xch[(w * 16 + row) * PITCH + pc + q];
-                if (SWIGLU) g[q] += xch[(w * 16 + row) * PITCH + pc + 16 + q];
+                v[q] += xch[(w * 16 + row) * PITCH + c + q];
+                if (SWIGLU) g[q] += xch[(w * 16 + row) * PITCH + c + 16 + q];
             }
         int crow = list0 + row;
         float sc = 1.f;
@@ -181,9 +179,9 @@ __global__ __launch_bounds__(kMx4SplitWaves * 64, 4) void mx4_split_kernel(Mx4Pr
                 const int row = EIGHTS == 1 ? l16 & 7 : l16;
                 a_lane[s] = mine_at + row * 128 + (((g16 * 2 + s) ^ swz(row)) * 16);
             }
-            f32x4 acc[1][2];
+            f32x4 acc[2];
 #pragma unroll
-            for (int j = 0; j < 2; ++j) acc[0][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int j = 0; j < 2; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
             Mx4Step t[2];
             auto load = [&](int i, auto B_tag) {  // step i of this wavefront's
                 constexpr int b = decltype(B_tag)::value;
@@ -218,8 +216,8 @@ __global__ __launch_bounds__(kMx4SplitWaves * 64, 4) void mx4_split_kernel(Mx4Pr
                 if constexpr (D == 1) load(i + 1, std::integral_constant<int, (b + 1) % 2>{});
                 static_for<8>([&](auto F) {
                     constexpr int f = decltype(F)::value, q = f / 2, s = f & 1;
-                    acc[0][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(step_values<q, s, 0>(t[b]), af[f], acc[0][0], 0, 0, 0);
-                    acc[0][1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(step_values<q, s, 1>(t[b]), af[f], acc[0][1], 0, 0, 0);
+                    acc[0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(step_values<q, s, 0>(t[b]), af[f], acc[0], 0, 0, 0);
+                    acc[1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(step_values<q, s, 1>(t[b]), af[f], acc[1], 0, 0, 0);
                 });
                 __builtin_amdgcn_sched_barrier(0);
                 if constexpr (D == 2) load(i + 2, std::integral_constant<int, b>{});
@@ -230,7 +228,7 @@ __global__ __launch_bounds__(kMx4SplitWaves * 64, 4) void mx4_split_kernel(Mx4Pr
             }
             wait_vmcnt<0>();  // (nothing that still writes LDS is under way)
             const int left = mt.rows - row0;
-            add_parts<1, EPI, false>(p, (float*)smem, wave, acc, mt.list0 + row0, left < 16 ? left : 16, panel);
+            add_parts<EPI, false>(p, (float*)smem, wave, acc, mt.list0 + row0, left < 16 ? left : 16, panel);
             __syncthreads();  // (the next unit's rows go to the same place)
         };
         if (mt.rows <= 8) unit(std::integral_constant<int, 1>{}, 0);
@@ -382,28 +380,22 @@ __global__ __launch_bounds__(512, 4) void mx4_wide_kernel(Mx4Product p) {
 
 template <int EPI>
 __global__ __launch_bounds__(kMx4SplitWaves * 64) void mx4_f32_kernel(Mx4Product p) {
-    constexpr int NG = 1, NW = kMx4SplitWaves;
-    __shared__ __align__(16) float xch[NW * 16 * (NG * kMx4N + 4)];
+    constexpr int NW = kMx4SplitWaves;
+    __shared__ __align__(16) float xch[NW * 16 * (kMx4N + 4)];
 
     const int tid = threadIdx.x;
     const int lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l16 = lane & 15, g16 = lane >> 4;
     const int KT = p.B.kt;
-    const int n_units = ceil_div(p.B.panels, NG);
-    const int total = p.counts[kCntEntries] * n_units;
+    const int total = p.counts[kCntEntries] * p.B.panels;
     const int kt0 = (int)((long long)KT * wave / NW), kt1 = (int)((long long)KT * (wave + 1) / NW);
     const size_t panel_bytes = mx4_panel_bytes(KT);
 
     for (int u = blockIdx.x; u < total; u += gridDim.x) {
-        const int entry = u / n_units, nu = u - entry * n_units;
+        const int entry = u / p.B.panels, panel = u - entry * p.B.panels;
         const MTile mt = p.mtiles[entry];
-        const unsigned char* panel[NG];
-#pragma unroll
-        for (int n = 0; n < NG; ++n) {  // (panels past the last repeat it, their columns are dropped)
-            const int at = nu * NG + n < p.B.panels ? nu * NG + n : p.B.panels - 1;
-            panel[n] = p.B.at + (size_t)mt.expert * p.B.expert + at * panel_bytes;
-        }
+        const unsigned char* const weights = p.B.at + (size_t)mt.expert * p.B.expert + panel * panel_bytes;
         auto unit = [&](auto MT_tag) {
             constexpr int MT = decltype(MT_tag)::value;  // 16-row groups of the M-tile that hold rows, rounded up
             const char* arow[MT];
@@ -413,16 +405,14 @@ __global__ __launch_bounds__(kMx4SplitWaves * 64) void mx4_f32_kernel(Mx4Product
                 r = row_at(p, mt.list0 + (r < mt.rows ? r : mt.rows - 1));
                 arow[i] = (const char*)p.A + (size_t)r * p.lda * 4;
             }
-            f32x4 acc[MT][NG][2];
+            f32x4 acc[MT][2];
 #pragma unroll
             for (int i = 0; i < MT; ++i)
 #pragma unroll
-                for (int n = 0; n < NG; ++n)
-#pragma unroll
-                    for (int j = 0; j < 2; ++j) acc[i][n][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+                for (int j = 0; j < 2; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
             struct Tile {
-                uint4 codes[NG];
-                unsigned scales[NG];
+                uint4 codes;
+                unsigned scales;
                 f32x4 a[MT][2][2];
             };
             // 16 bytes of a row from element k on, zeros past its end (what lies there is not this row's)
@@ -433,12 +423,8 @@ __global__ __launch_bounds__(kMx4SplitWaves * 64) void mx4_f32_kernel(Mx4Product
                 return v;
             };
             auto load = [&](int kt, Tile& t) {
-#pragma unroll
-                for (int n = 0; n < NG; ++n) {
-                    t.codes[n] = *(const uint4*)(panel[n] + mx4_codes_at(kt) + lane * 16);
-                    t.scales[n] = *(const unsigned short*)(panel[n] + mx4_scales_at(kt) + (g16 >> 1) * 128 + l16 * 8 +
-                                                           (kt & 3) * 2);
-                }
+                t.codes = *(const uint4*)(weights + mx4_codes_at(kt) + lane * 16);
+                t.scales = *(const unsigned short*)(weights + mx4_scales_at(kt) + (g16 >> 1) * 128 + l16 * 8 + (kt & 3) * 2);
 #pragma unroll
                 for (int i = 0; i < MT; ++i)
 #pragma unroll
@@ -451,12 +437,8 @@ __global__ __launch_bounds__(kMx4SplitWaves * 64) void mx4_f32_kernel(Mx4Product
             auto multiply = [&](const Tile& t) {
 #pragma unroll
                 for (int s = 0; s < 2; ++s) {
-                    bf16x8 b[NG][2];
-#pragma unroll
-                    for (int n = 0; n < NG; ++n) {
-                        b[n][0] = mx4_values(s ? t.codes[n].z : t.codes[n].x, mx4_scale<0>(t.scales[n]));
-                        b[n][1] = mx4_values(s ? t.codes[n].w : t.codes[n].y, mx4_scale<1>(t.scales[n]));
-                    }
+                    const bf16x8 b[2] = {mx4_values(s ? t.codes.z : t.codes.x, mx4_scale<0>(t.scales)),
+                                         mx4_values(s ? t.codes.w : t.codes.y, mx4_scale<1>(t.scales))};
 #pragma unroll
                     for (int i = 0; i < MT; ++i) {
                         bf16x8 a[3];
@@ -464,11 +446,8 @@ __global__ __launch_bounds__(kMx4SplitWaves * 64) void mx4_f32_kernel(Mx4Product
 #pragma unroll
                         for (int q = 0; q < 3; ++q)
 #pragma unroll
-                            for (int n = 0; n < NG; ++n)
-#pragma unroll
-                                for (int j = 0; j < 2; ++j)
-                                    acc[i][n][j] =
-                                        __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[n][j], a[q], acc[i][n][j], 0, 0, 0);
+                            for (int j = 0; j < 2; ++j)
+                                acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[j], a[q], acc[i][j], 0, 0, 0);
                     }
                 }
             };
@@ -484,7 +463,7 @@ __global__ __launch_bounds__(kMx4SplitWaves * 64) void mx4_f32_kernel(Mx4Product
             }
 #pragma unroll
             for (int i = 0; i < MT; ++i)
-                if (i * 16 < mt.rows) add_parts<NG, EPI, true>(p, xch, wave, acc[i], mt.list0 + i * 16, mt.rows - i * 16, nu);
+                if (i * 16 < mt.rows) add_parts<EPI, true>(p, xch, wave, acc[i], mt.list0 + i * 16, mt.rows - i * 16, panel);
         };
         if (mt.rows <= 16) unit(std::integral_constant<int, 1>{});
         else if (mt.rows <= 32) unit(std::integral_constant<int, 2>{});
