@@ -164,6 +164,33 @@ def test_packed_weights_past_32_bits(form):
         assert torch.equal(B.moe_unpack_matrix_mx4(packed, E, K, N, BF16), W)
 
 
+@pytest.mark.parametrize("gather", [False, True])
+def test_as_many_values_of_x_as_there_may_be(gather, dtype):
+    """2^31 - 4096 values of x (bf16: 2^32 bytes less 8192): its first and last rows, in place and through the permutation."""
+    E, K, N = 2, 4096, 40
+    rows = (2 ** 31 - 64) // K
+    gen = generator(3)
+    W = codes(gen, (E, K, N), dtype)
+    packed = B.moe_pack_matrix_mx4(W)
+    x = torch.zeros((rows, K), dtype=dtype, device="cuda")
+    x[:50], x[-300:] = whole(gen, (50, K), dtype), whole(gen, (300, K), dtype)
+    kw = {}
+    of = torch.arange(rows, device="cuda")
+    if gather:  # (back to front)
+        of = of.flip(0)
+        kw = dict(assign_of_row=of.to(torch.int32), k=1)
+    so, se = segments([200, rows - 250, 50], [0, 1, 0])
+    y = B.moe_grouped_product_mx4(x, so, se, packed, E, N, **kw)
+    expert = torch.ones(rows, dtype=torch.long, device="cuda")
+    expert[:200] = expert[-50:] = 0
+    loud = torch.cat([torch.arange(50, device="cuda"), torch.arange(rows - 300, rows, device="cuda")])
+    at = torch.argsort(of)[loud]  # places of those rows
+    for e in range(E):
+        mine = expert[at] == e
+        assert mine.any()
+        assert torch.equal(y[at[mine]], rounded(x[loud[mine]].double() @ W[e].double(), dtype))
+
+
 def test_second_matrices_past_32_bits(form):
     """An FFN whose second matrices lie behind the 2^32nd byte."""
     E, d, ffn = 640, 2048, 4096
