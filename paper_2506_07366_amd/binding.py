@@ -738,13 +738,16 @@ _PRODUCT_MX4_ARGS = struct.Struct("@8i2q8QQ")
 _FFN_MX4_ARGS = struct.Struct("@10i2q8QQ")
 
 
-def _rows_mx4(x: torch.Tensor, seg_offsets: torch.Tensor, slot_expert: torch.Tensor, width: int, seg_begin: int,
-              seg_end: Optional[int], assign_of_row: Optional[torch.Tensor], k: int, topk_w: Optional[torch.Tensor],
+def _rows_mx4(x: torch.Tensor, seg_offsets: torch.Tensor, slot_expert: torch.Tensor, width: Optional[int],
+              seg_begin: int, seg_end: Optional[int], assign_of_row: Optional[torch.Tensor], k: int, topk_w: Optional[torch.Tensor],
               out: Optional[torch.Tensor]):
-    """What both calls say about their rows: (dtype, A, rows of x, nseg, seg_end, k, out)."""
+    """What both calls say about their rows: (dtype, A, rows of x, nseg, seg_end, k, out).  width: of the results, None: x's."""
     dt = dtype_code(x)
     _need(x, x.dtype, "x")
+    if x.dim() != 2:
+        raise MoeGpsError(f"x must be [rows, width], got {list(x.shape)}")
     rows = x.shape[0]
+    width = x.shape[1] if width is None else width
     nseg = _need(slot_expert, torch.int32, "slot_expert").numel()
     if _need(seg_offsets, torch.int32, "seg_offsets").numel() != nseg + 1:
         raise MoeGpsError("seg_offsets must have one entry more than slot_expert")
@@ -791,9 +794,9 @@ def moe_grouped_ffn_mx4(x: torch.Tensor, seg_offsets: torch.Tensor, slot_expert:
                         workspace: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """y [A, d]: the experts' FFN with weights in 4 bits (``packed`` from moe_pack_weights_mx4).  ``x``: permuted rows
     [A, d], or with ``assign_of_row`` the tokens' rows [A / k, d].  ``topk_w``: gate weights that the results are multiplied by."""
-    d = x.shape[1]
-    dt, A, rows, nseg, seg_end, k, out = _rows_mx4(x, seg_offsets, slot_expert, d, seg_begin, seg_end, assign_of_row, k, topk_w,
+    dt, A, rows, nseg, seg_end, k, out = _rows_mx4(x, seg_offsets, slot_expert, None, seg_begin, seg_end, assign_of_row, k, topk_w,
                                                    out)
+    d = x.shape[1]
     _need_packed(packed, moe_packed_weights_mx4_bytes(E, d, ffn, relu), "packed")
     if workspace is None:
         workspace = torch.empty(moe_grouped_ffn_mx4_workspace_bytes(A, d, ffn, nseg, dt), dtype=torch.uint8, device=x.device)

@@ -244,3 +244,11 @@ def test_oracle_bounds():
     top = np.abs(w).reshape(10, 32, 50).max(1).repeat(32, 0)
     s = 2.0 ** np.ceil(np.log2(top / 6))
     assert (np.abs(q - w) <= np.maximum(0.2 * np.abs(w), s / 4) * (1 + 1e-12)).all()
+
+
+@pytest.mark.parametrize("fn", [B.moe_grouped_ffn_mx4, B.moe_grouped_product_mx4])
+@pytest.mark.parametrize("shape", [(4 * 64,), (4, 64, 2), (2, 4, 64)])
+def test_rows_of_another_rank(fn, shape):
+    """Only the first two sizes would be looked at, and less than all of x multiplied."""
+    with pytest.raises(B.MoeGpsError, match="x must be \\[rows, width\\]"):
+        call_python(fn, x=gpu(*shape))
