@@ -2,8 +2,13 @@
 //
 // Rows are tiled by expert, as in grouped_ffn.hip: the rows of all segments of an expert are listed one after the other by the table
 // builder (ffn_tables.h) and cut into M-tiles together.  Bound by the weights' bytes up to some 50 rows per expert, then by the matrix
-// pipe.  Both products, us, bf16 weights -> 4 bits: 128 tokens, top-8 of 128 experts of 4096 x 1536 503 -> 200, 16, top-2 of 8 of 4096 x
-// 14336 280 -> 121, 4096 2264 -> 2052 (1.41 PFLOP/s).
+// pipe; fp32 rows by neither (mx4_f32_kernel).  Both products and tables, us, bf16 weights -> 4 bits on the same batches: top-8 of 128
+// experts of 4096 x 1536, 1 token 59 -> 33, 128 391 -> 162, 1000 599 -> 372; top-2 of 8 of 4096 x 14336, 16 tokens 335 -> 118, 128
+// 471 -> 192, 1000 745 -> 606, 4096 2283 -> 2073 (1.39 PFLOP/s).
+//
+// With bf16 rows the hidden activation is rounded to bf16 between the products, as it is with bf16 weights: the second product takes bf16
+// operands, and a hidden row is half as long.  It doubles the error's square: results are 2.3 to 2.4e-3 from 64 bits in norm, where rounding
+// them alone makes 1.6 to 1.7e-3.  Kept in two bf16 parts it would double the second product's matrix instructions and the hidden rows.
 #include "mx4.h"
 
 namespace moegps {
@@ -74,6 +79,9 @@ constexpr int kFormRows[] = {kMx4SplitRows, kMx4WideRows, kMx4F32Rows, 0};  // o
 //   wide up to 24 rows per expert: 128 tokens, top-8 of 128 312 / 204 / 223, 64, top-2 of 8 232 / 179 / 216, 200, top-6 of 64 of 2048 x 1408
 //     147 / 79 / 88, but 512, top-8 of 128 - / 332 / 320, 777, top-6 of 64 - / 162 / 139; up to 128 where tiles would not
 //     go once round the chip: 400, top-4 of 16 of 4096 x 688, first product alone 46 / 30 / 40.
+// The rule sees the mean, not how the rows lie: where a few experts have nearly all of them it may choose the slower form.  rule / tiles, top-8 of
+// 128 experts of 4096 x 1536: 384 tokens on 95 of them (up to 257 rows) 283 / 280, on 32 (up to 346) 198 / 163, on 16 172 / 144; 128 tokens on
+// 32 (up to 117) 116 / 125, on 14 84 / 81; top-2 of 8 of 4096 x 14336, 96 tokens (96 rows on one) 124 / 144.
 // Hidden rows of 2^31 values and more are left to the tiles, which address them from the tile's first row; the others have 32-bit
 // offsets into all of them.  values: of the product's rows.
 static Mx4Form form_of(int opt, int dtype, int64_t A, int E, const Mx4Matrix& m, int64_t values) {

@@ -7,8 +7,8 @@
 //
 // Bound by memory: 2 (fp32: 4) bytes of a weight one way and 0.53 the other.  A workgroup of four wavefronts turns a k-tile of eight
 // panels: a lane takes two neighbouring columns of a matrix and 32 of k, a row's pieces of a wavefront being 256 (512) contiguous
-// bytes, all of its 32 rows under way at once (8 experts of 4096 x 14336, there and back 1317 us, 5.4 TB/s); a group's maximum is then the lane's own.  The codes meet in LDS in the order of the
-// layout and leave as whole kilobytes.
+// bytes, all of its 32 rows under way at once; a group's maximum is then the lane's own.  The codes meet in LDS in the order of the
+// layout and leave as whole kilobytes.  8 experts of 4096 x 14336 680 us there, 659 back (5.3 TB/s); 8 of 128 x 256 10 and 11, two launches each.
 #include "mx4.h"
 
 namespace moegps {

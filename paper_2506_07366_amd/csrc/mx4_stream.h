@@ -239,7 +239,8 @@ __global__ __launch_bounds__(kMx4SplitWaves * 64, 4) void mx4_split_kernel(Mx4Pr
 
 // For many units of few rows: eight panels side by side, one per wavefront, over all of K, and up to 32 rows, which the wavefronts share
 // in LDS: three steps of them, one barrier a step.  128 tokens on 128 experts of 4096 x 1536 122 us (4.6 TB/s) and 69; nothing but the loads
-// of the weights would take three quarters of that.  Units of 32 rows cost more than their bytes, those of 16 do not.
+// of the weights would take three quarters of that.  Units of 32 rows cost more than their bytes, those of 16 do not.  Two workgroups a CU leave 128
+// registers: 21 to 40 values of a lane that hold for a unit are in scratch, stored at entry and reloaded ahead of the K loop and behind it, not in it.
 constexpr int kMx4WideRows = 32, kMx4WideDepth = 3;
 constexpr int kMx4WideStage = kMx4WideRows * kStepK * 2;
 constexpr size_t kMx4WideLds = (size_t)kMx4WideDepth * kMx4WideStage;
@@ -378,6 +379,10 @@ __global__ __launch_bounds__(512, 4) void mx4_wide_kernel(Mx4Product p) {
     }
 }
 
+// One form for every fp32 batch, right and far from a floor of three bf16 products: for each panel of 32 columns a workgroup loads its rows from
+// global memory again and cuts them into parts again, some 200 vector instructions to 12 matrix instructions of 16 rows and a k-tile (counted in
+// the source).  FFN of 8 experts of 1024 x 2048, 256 tokens 131 us (floor 16), 4096 tokens 1459 to 1513 (261; fp32 weights 1658); 64 of 2048 x
+// 1408, 2048 tokens 2790 to 2804 (539); 16 tokens on 128 of 4096 x 1536 248 (79, 1.6 TB/s).
 template <int EPI>
 __global__ __launch_bounds__(kMx4SplitWaves * 64) void mx4_f32_kernel(Mx4Product p) {
     constexpr int NW = kMx4SplitWaves;
