@@ -231,7 +231,7 @@ def prepare(case, seed):
         E, d, ffn, dt = case["experts"], case["d"], case["ffn"], DTYPES[case["dtype"]]
         relu = case["act"] == "relu"
         if case["op"] == "weights":
-            state["packed"] = B.moe_pack_weights_mx4(state["W1"], state.get("W3"), state["W2"])
+            state["packed"] = torch.empty(B.moe_packed_weights_mx4_bytes(E, d, ffn, relu), dtype=torch.uint8, device="cuda")
             state["back"] = tuple(torch.empty_like(state[w]) if w in state else None for w in ("W1", "W3", "W2"))
             return state
         # weights are packed once, as a layer is loaded; results go to buffers that the program keeps
